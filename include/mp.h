@@ -381,6 +381,122 @@ mp_status mp_dense_attention_static(const void* q, const void* k, const void* v,
                                     int32_t n_q_heads, int32_t n_kv_heads, int32_t n, float softmax_scale,
                                     void* out, float* lse, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Before the index: rotary positions and a paged cache that a prompt is read into, piece by piece.
+ *
+ *   mp_paged_append      new tokens join the cache, keys (and their queries) rotated on the way
+ *   mp_paged_attention   the new tokens attend all that the cache holds of their sequence
+ *   mp_paged_gather      a sequence's rows in order: what mp_cluster_kv and mp_local_buffer_init take
+ *   mp_rotary            rotary positions by themselves: what mp_decode_step takes per token
+ *
+ * All are context-free (errors through mp_last_error(NULL)), run on the current device, allocate
+ * nothing, wait for nothing and read nothing back.  Their kernels take lengths, starts and page
+ * tables from device memory, so a captured graph follows them as they change.  Rows of 128 bf16
+ * elements start on 16 bytes; "token stride": elements between one token's rows and the next one's (a multiple of 8, at least the
+ * token's rows; 0: densely packed), so that the rows of a fused projection are read in place.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Rotary positions: of every pair (x0, x1) among the first rot_dim dimensions of a head, at position p,
+ *   y0 = A (x0 cos(p f) - x1 sin(p f)),   y1 = A (x1 cos(p f) + x0 sin(p f)),
+ * f = freqs[pair], pair = 0 .. rot_dim/2 - 1.  The other dimensions stay as they are.  Angles are
+ * worked out in fp64, the rest in fp32, rounded to bf16 once.  Positions may be negative: the same call
+ * with every position negated is the gradient with respect to x. */
+#define MP_ROTARY_HALF 0          /* pairs (i, i + rot_dim/2)      */
+#define MP_ROTARY_INTERLEAVED 1   /* pairs (2 i, 2 i + 1)          */
+typedef struct {
+    const double* freqs;   /* device fp64 [rot_dim / 2], radians a position                           */
+    int32_t rot_dim;       /* even, 2 .. 128                                                          */
+    int32_t layout;        /* MP_ROTARY_HALF or MP_ROTARY_INTERLEAVED                                 */
+    float amplitude;       /* A, finite; 1 unless a context extension scales queries and keys         */
+} mp_rotary_spec;
+
+/* The usual frequencies, host fp64 [rot_dim / 2]; no GPU work.
+ *   MP_ROTARY_PLAIN     f_i = base^(-2 i / rot_dim)
+ *   MP_ROTARY_LINEAR    f_i / factor (positions interpolated)
+ *   MP_ROTARY_BASE      the plain ones of base * factor^(rot_dim / (rot_dim - 2))
+ *   MP_ROTARY_BY_PARTS  a pair that turns r = original_len f_i / 2 pi times over the original length keeps the share
+ *                       g = clamp((r - low) / (high - low), 0, 1) of its frequency: g f_i + (1 - g) f_i / factor
+ * Arguments that a scaling does not name are ignored.  Errors: MP_EINVAL. */
+#define MP_ROTARY_PLAIN 0
+#define MP_ROTARY_LINEAR 1
+#define MP_ROTARY_BASE 2
+#define MP_ROTARY_BY_PARTS 3
+mp_status mp_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                                double low, double high, double* freqs);
+
+/* mp_rotary -- rows turned to their positions, and to one fixed position (lookup keys and queries).
+ *   x            device bf16 [n_tokens, n_heads, 128], token stride x_stride
+ *   positions    device int32 [n_tokens]; may be NULL without `out`
+ *   out          device bf16, token stride out_stride; may be x itself (same stride), or NULL
+ *   out_lookup   device bf16 [n_tokens, n_heads, 128], every row turned to lookup_position instead; or NULL
+ * Outputs overlap neither each other nor x, but for `out` (or, x densely packed, out_lookup) in x's place.
+ * Errors: MP_EINVAL, MP_EHIP. */
+mp_status mp_rotary(const mp_rotary_spec* rotary, const void* x, int64_t x_stride, const int32_t* positions,
+                    int32_t n_tokens, int32_t n_heads, void* out, int64_t out_stride, void* out_lookup,
+                    int32_t lookup_position, void* stream);
+
+/* The paged cache and a batch of sequences over it.  Key j of sequence b lies in row j % page_size of page
+ * page_table[b][j / page_size].  An entry outside [0, n_pages) stands for no page: its keys are attended by no one,
+ * appended rows for it are dropped, gathered rows of it are zero.  Sequences may share pages that are only read.
+ * The new tokens of a call are the rows [q_start[b], q_start[b+1]) of its tensors for sequence b (q_start does not decrease); they are the
+ * last ones of its kv_len[b] keys, so token i of n stands at position kv_len[b] - n + i.  Rows before q_start[0] and
+ * behind q_start[n_seqs] belong to no sequence: their outputs are left as they were.  Nothing else is ever read of the
+ * pages than the rows of kv_len[b] keys; the rest of a page may hold anything. */
+typedef struct {
+    void* k_pages;               /* device bf16 [n_pages, n_kv_heads, page_size, 128]                 */
+    void* v_pages;               /* likewise                                                          */
+    const int32_t* page_table;   /* device int32 [n_seqs, table_stride]                               */
+    const int32_t* kv_len;       /* device int32 [n_seqs]: keys of each sequence, the new ones among them */
+    const int32_t* q_start;      /* device int32 [n_seqs + 1]                                         */
+    int32_t n_pages;
+    int32_t page_size;           /* a power of two, 1 .. 1024                                         */
+    int32_t n_kv_heads;
+    int32_t head_dim;            /* must be 128                                                       */
+    int32_t n_seqs;
+    int32_t table_stride;        /* entries of a sequence in page_table (times page_size below 2^31)  */
+} mp_paged_kv;
+
+/* mp_paged_append -- store the new tokens' keys, turned to their positions, and values; optionally turn
+ * their queries in the same launch.
+ *   rotary     NULL: keys (and queries) are stored as they come
+ *   q, q_out   device bf16 [n_tokens, n_q_heads, 128], q with a token stride, q_out densely packed (it may be q if that is,
+ *              too); both NULL: keys and values only
+ *   k, v       device bf16 [n_tokens, n_kv_heads, 128] with token strides
+ *   n_tokens   rows of the tensors (>= q_start[n_seqs]; rows past that are not read)
+ * Tokens at a negative position, behind the table's end or without a page are dropped (their queries are turned all the same).
+ * Two tokens for the same row of a page leave it unspecified.  Errors: MP_EINVAL, MP_EHIP. */
+mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary, const void* q, int64_t q_stride,
+                          int32_t n_q_heads, void* q_out, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int32_t n_tokens, void* stream);
+
+/* mp_paged_attention -- every new token attends the keys of its sequence up to its own.
+ *   q               device bf16 [n_tokens, n_q_heads, 128] with a token stride
+ *   max_new         no sequence has more new tokens (rows past that are left as they were); 0: n_tokens.  It
+ *                   says which kernels run: a decode step passes 1.
+ *   window          a token attends its last `window` keys, itself among them; 0: all
+ *   softmax_scale   0 => 1/sqrt(128)
+ *   out             device bf16 [n_tokens, n_q_heads, 128]
+ *   lse             device fp32 [n_tokens, n_q_heads], natural log of the softmax denominator; may be NULL
+ *   workspace       device buffer of at least mp_paged_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, n_seqs,
+ *                   max_new) bytes on a 16-byte boundary; it need not be cleared, and calls that may overlap on the GPU
+ *                   need one each
+ * A token that attends no key (position below zero, pages missing) gets zeros and -inf.  1 <= G <= 8.  fp32 accumulation
+ * of bf16 products; probabilities are rounded to bf16 for their product with the values.
+ * Errors: MP_EINVAL, MP_EHIP. */
+size_t mp_paged_workspace_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t max_new);
+mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_stride, int32_t n_tokens,
+                             int32_t n_q_heads, int32_t max_new, int32_t window, float softmax_scale, void* out,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* mp_paged_gather -- keys and values [first, first + n) of every sequence in order; rows that a sequence does not hold are
+ * zero.  q_start is not used.
+ *   k, k_lookup, v   device bf16 [n_seqs, n_kv_heads, n, 128]; each may be NULL, one is not
+ *   k_lookup         the stored keys turned on from their position to lookup_position, without another amplitude
+ *                    (`rotary`: what they were stored with; it may be NULL without k_lookup)
+ * Errors: MP_EINVAL, MP_EHIP. */
+mp_status mp_paged_gather(const mp_paged_kv* cache, const mp_rotary_spec* rotary, int32_t first, int32_t n,
+                          int32_t lookup_position, void* k, void* k_lookup, void* v, void* stream);
+
 /* Library version string. */
 const char* mp_version(void);
 

@@ -22,10 +22,13 @@ EXPORTS = [
     "mp_set_clustering", "mp_update_clusters", "mp_decode_attention", "mp_get_sizes", "mp_get_assignments",
     "mp_get_centroids", "mp_get_selection", "mp_get_counters", "mp_get_layout", "mp_dense_workspace_bytes",
     "mp_dense_attention", "mp_version", "mp_enable_stage_timing", "mp_get_stage_timing", "mp_update_seed_counts", "mp_local_buffer_init", "mp_local_buffer_size", "mp_decode_step",
-    "mp_dense_static_scratch_bytes", "mp_dense_attention_static", "mp_get_kv_codes",
+    "mp_dense_static_scratch_bytes", "mp_dense_attention_static", "mp_get_kv_codes", "mp_rotary_frequencies", "mp_rotary",
+    "mp_paged_append", "mp_paged_attention", "mp_paged_gather", "mp_paged_workspace_bytes",
 ]
 
 MP_KV_BF16, MP_KV_E4M3 = 0, 1
+MP_ROTARY_HALF, MP_ROTARY_INTERLEAVED = 0, 1
+MP_ROTARY_PLAIN, MP_ROTARY_LINEAR, MP_ROTARY_BASE, MP_ROTARY_BY_PARTS = range(4)
 
 
 class MpError(RuntimeError):
@@ -38,6 +41,15 @@ class MpConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "batch", "n_q_heads", "n_kv_heads", "head_dim", "max_tokens", "levels", "max_fine", "max_coarse",
         "block_w", "block_alpha", "max_tail", "lookup_keys")] + [("softmax_scale", C.c_float), ("kv_format", C.c_int32)]
+
+
+class MpRotarySpec(C.Structure):
+    _fields_ = [("freqs", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float)]
+
+
+class MpPagedKvArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_pages", "v_pages", "page_table", "kv_len", "q_start")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "n_seqs", "table_stride")]
 
 
 _lib = None
@@ -86,6 +98,14 @@ def lib():
         L.mp_dense_static_scratch_bytes.argtypes = []
         L.mp_dense_static_scratch_bytes.restype = sz
         L.mp_dense_attention_static.argtypes = [vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp]
+        i64, f64 = C.c_int64, C.c_double
+        L.mp_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp]
+        L.mp_rotary.argtypes = [vp, vp, i64, vp, i32, i32, vp, i64, vp, i32, vp]
+        L.mp_paged_append.argtypes = [vp, vp, vp, i64, i32, vp, vp, i64, vp, i64, i32, vp]
+        L.mp_paged_attention.argtypes = [vp, vp, i64, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.mp_paged_gather.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp]
+        L.mp_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.mp_paged_workspace_bytes.restype = sz
         _lib = L
     return _lib
 
@@ -158,6 +178,172 @@ def mp_dense_attention_static(q, k, v, out, lse=None, softmax_scale=0.0):
                                          _stream())
     _check(st)
     return out
+
+
+def _reject(msg):
+    raise MpError(MP_EINVAL, msg)
+
+
+def _on_device(t, name, dtype, dims=None):
+    """A tensor of a call on the current device: its type and number of dimensions are what the kernels take them to be."""
+    if t.dtype is not dtype or not t.is_cuda or t.device.index != torch.cuda.current_device() or (dims is not None and t.dim() != dims):
+        _reject(f"{name}: {dtype}{'' if dims is None else f' of {dims} dimensions'} on the current device expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
+def _dense(t, name, dtype, shape):
+    _on_device(t, name, dtype)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _reject(f"{name}: a contiguous tensor {tuple(shape)} expected, got {tuple(t.shape)} with strides {t.stride()}")
+    return t
+
+
+def _token_rows(t, name):
+    """(tokens, heads, token stride) of a bf16 tensor [tokens, heads, 128] whose tokens may be apart, as in the rows of a fused projection."""
+    _on_device(t, name, torch.bfloat16, 3)
+    n, h, d = t.shape
+    s0, s1, s2 = t.stride()
+    if d != 128 or s2 != 1 or (h > 1 and s1 != 128):
+        _reject(f"{name}: [tokens, heads, 128] with each token's rows behind one another expected, got {(n, h, d)} with strides {(s0, s1, s2)}")
+    return n, h, s0 if n > 1 else 0
+
+
+def mp_rotary_frequencies(rot_dim=128, base=10000.0, scaling=MP_ROTARY_PLAIN, factor=1.0, original_len=0.0, low=1.0, high=32.0):
+    """fp64 CPU tensor [rot_dim / 2]: radians a position of every pair."""
+    out = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
+    _check(lib().mp_rotary_frequencies(rot_dim, base, scaling, factor, original_len, low, high, out.data_ptr()))
+    return out
+
+
+class MpRotary:
+    """Rotary positions: frequencies on the current device (given, or worked out by mp_rotary_frequencies), layout and amplitude."""
+
+    def __init__(self, rot_dim=128, layout=MP_ROTARY_HALF, base=10000.0, scaling=MP_ROTARY_PLAIN, factor=1.0, original_len=0.0, low=1.0, high=32.0,
+                 amplitude=1.0, freqs=None):
+        if freqs is None:
+            freqs = mp_rotary_frequencies(rot_dim, base, scaling, factor, original_len, low, high).cuda()
+        self.freqs = _dense(freqs, "freqs", torch.float64, (rot_dim // 2,))
+        self.spec = MpRotarySpec(self.freqs.data_ptr(), rot_dim, layout, amplitude)
+        self.at = C.addressof(self.spec)
+
+    def _at(self, device):
+        if self.freqs.device != device:
+            _reject(f"the frequencies lie on {self.freqs.device}, the tensors on {device}")
+        return self.at
+
+    def mp_rotary(self, x, positions=None, out=None, lookup_position=None, out_lookup=None):
+        """x bf16 [tokens, heads, 128] at positions int32 [tokens] -> out (like x, densely packed; `out` may be x).  With a lookup_position:
+        (out, out_lookup), out_lookup turned to that one position; positions may then be None for the second alone."""
+        n, h, stride = _token_rows(x, "x")
+        to_stride = 0
+        if positions is not None:
+            _dense(positions, "positions", torch.int32, (n,))
+            if out is None:
+                out = torch.empty(n, h, 128, dtype=torch.bfloat16, device=x.device)
+            else:
+                no, ho, to_stride = _token_rows(out, "out")
+                if (no, ho) != (n, h):
+                    _reject(f"out: [{n}, {h}, 128] expected, got {tuple(out.shape)}")
+        elif out is not None or lookup_position is None:
+            _reject("positions are missing")
+        if lookup_position is not None:
+            if out_lookup is None:
+                out_lookup = torch.empty(n, h, 128, dtype=torch.bfloat16, device=x.device)
+            _dense(out_lookup, "out_lookup", torch.bfloat16, (n, h, 128))
+        elif out_lookup is not None:
+            _reject("out_lookup needs a lookup_position")
+        st = lib().mp_rotary(self._at(x.device), x.data_ptr(), stride, None if positions is None else positions.data_ptr(), n, h,
+                             None if out is None else out.data_ptr(), to_stride, None if out_lookup is None else out_lookup.data_ptr(),
+                             lookup_position or 0, _stream())
+        _check(st)
+        return out if lookup_position is None else (out, out_lookup)
+
+
+def mp_paged_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, n_seqs, max_new):
+    return int(lib().mp_paged_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, n_seqs, max_new))
+
+
+class MpPagedKv:
+    """A batch of sequences over a paged cache: k_pages, v_pages bf16 [n_pages, Hkv, page_size, 128], page_table int32 [n_seqs, pages],
+    kv_len int32 [n_seqs], q_start int32 [n_seqs + 1].  The tensors are kept, not copied: change them in place between calls."""
+
+    def __init__(self, k_pages, v_pages, page_table, kv_len, q_start):
+        _on_device(k_pages, "k_pages", torch.bfloat16, 4)
+        n_pages, self.n_kv_heads, page_size, d = k_pages.shape
+        _dense(k_pages, "k_pages", torch.bfloat16, k_pages.shape)
+        _dense(v_pages, "v_pages", torch.bfloat16, k_pages.shape)
+        _on_device(page_table, "page_table", torch.int32, 2)
+        self.n_seqs = page_table.shape[0]
+        _dense(page_table, "page_table", torch.int32, page_table.shape)
+        _dense(kv_len, "kv_len", torch.int32, (self.n_seqs,))
+        _dense(q_start, "q_start", torch.int32, (self.n_seqs + 1,))
+        self.tensors = (k_pages, v_pages, page_table, kv_len, q_start)
+        self.device = k_pages.device
+        self.args = MpPagedKvArgs(*(t.data_ptr() for t in self.tensors), n_pages, page_size, self.n_kv_heads, d, self.n_seqs, page_table.shape[1])
+        self.at = C.addressof(self.args)
+
+    def _here(self):
+        if self.device.index != torch.cuda.current_device():
+            _reject(f"the cache lies on {self.device}, not on the current device")
+
+    def mp_paged_append(self, k, v, rotary=None, q=None, q_out=None):
+        """k, v bf16 [tokens, Hkv, 128] join the cache; returns the turned queries q_out [tokens, Hq, 128], or None without q."""
+        self._here()
+        n, h, ks = _token_rows(k, "k")
+        nv, hv, vs = _token_rows(v, "v")
+        if h != self.n_kv_heads or (nv, hv) != (n, h):
+            _reject(f"k, v: [tokens, {self.n_kv_heads}, 128] expected, got {tuple(k.shape)} and {tuple(v.shape)}")
+        hq = qs = 0
+        if q is not None:
+            nq, hq, qs = _token_rows(q, "q")
+            if nq != n:
+                _reject(f"q: {n} tokens expected, got {nq}")
+            if q_out is None:
+                q_out = torch.empty(n, hq, 128, dtype=torch.bfloat16, device=q.device)
+            _dense(q_out, "q_out", torch.bfloat16, (n, hq, 128))
+        elif q_out is not None:
+            _reject("q_out needs q")
+        st = lib().mp_paged_append(self.at, None if rotary is None else rotary._at(self.device), None if q is None else q.data_ptr(), qs, hq,
+                                   None if q_out is None else q_out.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, n, _stream())
+        _check(st)
+        return q_out
+
+    def mp_paged_attention(self, q, max_new=0, window=0, softmax_scale=0.0, out=None, lse=None, workspace=None):
+        """q bf16 [tokens, Hq, 128] -> out bf16 [tokens, Hq, 128] (and lse fp32 [tokens, Hq]); max_new: as many new tokens a sequence at most."""
+        self._here()
+        n, hq, qs = _token_rows(q, "q")
+        if out is None:
+            out = torch.empty(n, hq, 128, dtype=torch.bfloat16, device=q.device)
+        _dense(out, "out", torch.bfloat16, (n, hq, 128))
+        if lse is not None:
+            _dense(lse, "lse", torch.float32, (n, hq))
+        if workspace is None:
+            workspace = torch.empty(mp_paged_workspace_bytes(n, hq, self.n_kv_heads, self.n_seqs, max_new), dtype=torch.uint8, device=q.device)
+        else:
+            _on_device(workspace, "workspace", workspace.dtype)
+        st = lib().mp_paged_attention(self.at, q.data_ptr(), qs, n, hq, max_new, window, softmax_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                      _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
+        _check(st)
+        return out
+
+    def mp_paged_gather(self, n, first=0, rotary=None, lookup_position=None, k=None, v=None, k_lookup=None):
+        """Keys and values [first, first + n) of every sequence: (k, v) bf16 [n_seqs, Hkv, n, 128], with a lookup_position (k, v, k_lookup)."""
+        self._here()
+        shape = (self.n_seqs, self.n_kv_heads, n, 128)
+        if n < 0:
+            _reject(f"n = {n} < 0")
+        k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.device) if t is None else _dense(t, "k, v", torch.bfloat16, shape) for t in (k, v))
+        if lookup_position is not None:
+            if rotary is None:
+                _reject("a lookup_position needs the rotary that the keys were stored with")
+            k_lookup = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if k_lookup is None else _dense(k_lookup, "k_lookup", torch.bfloat16, shape)
+        elif k_lookup is not None:
+            _reject("k_lookup needs a lookup_position")
+        if n > 0:
+            st = lib().mp_paged_gather(self.at, None if rotary is None else rotary._at(self.device), first, n, lookup_position or 0, k.data_ptr(),
+                                       None if k_lookup is None else k_lookup.data_ptr(), v.data_ptr(), _stream())
+            _check(st)
+        return (k, v) if lookup_position is None else (k, v, k_lookup)
 
 
 class MpContext:
