@@ -25,4 +25,24 @@ MP_PAGE_FN long long row_of(int page, int head, int n_kv, int page_shift, int po
     return (((long long)page * n_kv + head) << page_shift) + (position & ((1 << page_shift) - 1));
 }
 
+// Blocks of `unit` keys that tokens [i0, i1] of a sequence attend (token i stands at position base + i): [b0, b1), one at least, so that
+// rows without a key are someone's, too.  `room`: keys that the table has entries for.
+MP_PAGE_FN void blocks_of(int base, int i0, int i1, int window, int room, int unit, int* b0, int* b1)
+{
+    const int end = base + i1 + 1 < room ? base + i1 + 1 : room;
+    const int low = window > 0 && base + i0 >= window ? base + i0 - window + 1 : 0;
+    *b0 = low / unit;
+    *b1 = end > 0 ? (int)(((long long)end + unit - 1) / unit) : 0;
+    if (*b1 <= *b0) *b1 = *b0 + 1;
+}
+
+// Work is cut into equal shares of blocks, a workgroup each, without regard to where an item (a tile of rows of a head) ends; the first
+// and the last item of a share may be parts.  Which workgroup holds what of the item [x0, x1):
+struct Parts {
+    long long first, last;      // workgroups
+};
+MP_PAGE_FN Parts parts_of(long long x0, long long x1, long long share) { return Parts{x0 / share, (x1 - 1) / share}; }
+// ... and in which of a workgroup's two slots: what it begins with, or what it ends with.
+MP_PAGE_FN int slot_of(long long x0, long long workgroup, long long share) { return x0 > workgroup * share ? 1 : 0; }
+
 }  // namespace mp

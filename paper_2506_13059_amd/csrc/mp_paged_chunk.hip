@@ -1,0 +1,414 @@
+// Attention of many new tokens over a paged cache, on the matrix cores, for gfx950.  (mp_paged_attn.hip says what is computed.)
+//
+// Eight waves of 32 query rows each work on one item (mp_paged_plan.h): 64 keys and values at a time are brought to LDS by all of them, through registers, a block
+// ahead.  S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16, so a lane holds one query row in both (its column): its softmax
+// needs no more of other lanes than one exchange of maxima, and the rows of S^T that it holds are, converted to bf16, what the second product takes from it,
+// with the values' rows read (transposed by LDS) in the same order.
+#include "mp_paged_plan.h"
+
+namespace mp {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+constexpr int kWaves = 8, kKeys = 64, kRows = 32 * kWaves;
+constexpr int kBlockBytes = kKeys * 256;
+constexpr int kWorkgroups = 256;
+constexpr int kPartFloats = kRows * kHeadDim + 2 * kRows;       // a part: weighted values as the lanes hold them, then maxima, then sums
+
+template <typename T>
+__device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t at)
+{
+    return reinterpret_cast<__attribute__((address_space(3))) T*>((uintptr_t)at);
+}
+__device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(lds_byte*)p; }
+
+struct Softmax {
+    f32x16 o[4];             // rows of block d: dims 32 d + 8 (i / 4) + 4 (lane / 32) + i % 4
+    float m, l;              // of this lane's query row, m in powers of two; l of the keys that the lane has seen
+};
+
+__device__ __forceinline__ float over_halves_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float over_halves_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ void workgroup_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The rows of a finished item.
+__device__ __forceinline__ void store_rows(const PagedAttention& a, const Softmax& st, float l, int token, int head, bool there)
+{
+    const int half = (threadIdx.x & 63) >> 5;
+    if (!there) return;
+    const float f = l > 0.f ? 1.f / l : 0.f;
+    const long long row = (long long)token * a.n_q_heads + head;
+    unsigned char* out = reinterpret_cast<unsigned char*>(a.out) + row * 256 + half * 8;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bf16x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (__bf16)(l > 0.f ? st.o[d][4 * j + e] * f : 0.f);
+            *reinterpret_cast<bf16x4*>(out + d * 64 + j * 16) = w;
+        }
+    if (a.lse && half == 0) a.lse[row] = l > 0.f ? (st.m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+}
+
+__device__ __forceinline__ void store_part(float* part, const Softmax& st, float l)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    f32x4* o = reinterpret_cast<f32x4*>(part) + wave * 16 * 64 + lane;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[(4 * d + j) * 64] = f32x4{st.o[d][4 * j], st.o[d][4 * j + 1], st.o[d][4 * j + 2], st.o[d][4 * j + 3]};
+    if (lane < 32) {
+        part[kRows * kHeadDim + wave * 32 + lane] = st.m;
+        part[kRows * kHeadDim + kRows + wave * 32 + lane] = l;
+    }
+}
+
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts)
+{
+    __shared__ __align__(256) unsigned char lds_k[2][kBlockBytes];
+    __shared__ __align__(256) unsigned char lds_v[2][kBlockBytes];
+    __shared__ __align__(8) unsigned char lds_valid[2][kWaves];      // keys that are there, a bit each
+    __shared__ __align__(8) unsigned char lds_odd[2][kWaves];        // ... of an edge's block, whose values are not all finite
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+    const Line line = line_of(a, tl);
+    const int share = share_of(line, blockIdx.x);
+    if (share < 0) return;
+    const float scale = a.scale_log2e;
+    const int G = tl.group;
+
+    // LDS addresses: of the lane's row in the first 32 keys, chunk 2 ks + half; of its place in the first 16 values, dims 32 d
+    uint32_t k_at[8], v_at[4];
+    {
+        const int row = lane & 31, v_row = 4 * half + ((lane & 15) >> 2);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) k_at[ks] = lds_offset(lds_k) + row * 256 + (((2 * ks + half) ^ (row & 15)) << 4);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+            v_at[d] = lds_offset(lds_v) + v_row * 256 + (((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ ((v_row & 3) << 2)) << 4) + (lane & 1) * 8;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(k_at[ks]));
+#pragma unroll
+        for (int d = 0; d < 4; ++d) asm volatile("" : "+v"(v_at[d]));
+    }
+
+    long long x = share * line.share;
+    const long long x_end = min(x + line.share, line.all);
+    while (x < x_end) {
+        const int h = (int)(x / line.of_head);
+        Item it;
+        walk<true>(a, tl, (uint32_t)(x - (long long)h * line.of_head), &it);
+        const int first = it.b0 + (int)((uint32_t)(x - (long long)h * line.of_head) - it.before);
+        const int last = (int)min((long long)it.b1, first + (x_end - x));
+        const bool whole = first == it.b0 && last == it.b1;
+
+        // this lane's query row
+        const int tile_rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * G;
+        const int r = min(wave * 32 + (lane & 31), tile_rows - 1);
+        const int i = it.tile * tl.tokens + r / G, head = h * G + r % G;
+        const int position = it.rows.base + i;
+        const bool active = wave * 32 < tile_rows;
+        const int pos_min = lane_value(position, 0), pos_max = lane_value(position, 31);
+        bf16x8 q[8];
+        {
+            const uint4* from = reinterpret_cast<const uint4*>(a.q + (long long)(it.rows.q0 + i) * a.q_stride + (long long)head * kHeadDim);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(bf16x8, from[2 * ks + half]);
+        }
+
+        // Loading: rows 8 wave + 4 e + lane / 16 of a block, chunk lane % 16 of 16 bytes.  In LDS chunk j of row k lies at j ^ k % 16 (keys) or j ^ 4 (k % 4)
+        // (values): what the lanes of a read touch together lies in different banks.
+        const int32_t* entries = a.c.table + (long long)it.b * a.c.table_stride;
+        const int chunk = lane & 15;
+        const int end = min(it.rows.base + it.rows.n, room_of(a));       // keys of the sequence
+        auto page_at = [&](int block, int e) {
+            const int key = block * kKeys + 8 * wave + 4 * e + (lane >> 4);
+            return key < end ? page_of(entries, a.c.table_stride, a.c.n_pages, a.c.page_shift, key) : -1;
+        };
+        auto offset_at = [&](int block, int e, int page) {
+            return row_of(max(page, 0), h, a.c.n_kv, a.c.page_shift, block * kKeys + 8 * wave + 4 * e + (lane >> 4)) * 16 + chunk;
+        };
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+        auto load = [&](const uint16_t* base, int block, const int (&page)[2], uint4 (&w)[2]) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                w[e] = zero;
+                if (page[e] >= 0) w[e] = reinterpret_cast<const uint4*>(base)[offset_at(block, e, page[e])];
+            }
+        };
+        auto store_k = [&](int block, const int (&page)[2], const uint4 (&w)[2]) {
+            uint32_t bits = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = 8 * wave + 4 * e + (lane >> 4);
+                *reinterpret_cast<uint4*>(&lds_k[block & 1][row * 256 + ((chunk ^ (row & 15)) << 4)]) = w[e];
+                const unsigned long long in = __ballot(page[e] >= 0);
+                bits |= ((uint32_t)(in & 1) | (uint32_t)(in >> 15 & 2) | (uint32_t)(in >> 30 & 4) | (uint32_t)(in >> 45 & 8)) << (4 * e);
+            }
+            if (lane == 0) lds_valid[block & 1][wave] = (unsigned char)bits;
+        };
+        // a block in which some row of the item sees a key that another one does not
+        auto edge = [&](int block) {
+            return block * kKeys + kKeys - 1 > it.rows.base + it.tile * tl.tokens ||
+                   (a.window && block * kKeys <= it.rows.base + min(it.rows.n, (it.tile + 1) * tl.tokens) - 1 - a.window);
+        };
+        auto store_v = [&](int block, uint4 (&w)[2]) {
+            uint32_t bits = 0;
+            if (edge(block)) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
+                    bool odd = false;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool lo = (u[k] & 0x7f80u) == 0x7f80u, hi = (u[k] & 0x7f800000u) == 0x7f800000u;
+                        odd |= lo | hi;
+                        u[k] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                    }
+                    w[e] = make_uint4(u[0], u[1], u[2], u[3]);
+                    const unsigned long long in = __ballot(odd);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) bits |= (uint32_t)((in >> (16 * k) & 0xffff) != 0) << (4 * e + k);
+                }
+            }
+            if (lane == 0) lds_odd[block & 1][wave] = (unsigned char)bits;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = 8 * wave + 4 * e + (lane >> 4);
+                *reinterpret_cast<uint4*>(&lds_v[block & 1][row * 256 + ((chunk ^ ((row & 3) << 2)) << 4)]) = w[e];
+            }
+        };
+
+        auto scores = [&](int block, f32x16 (&s)[2]) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    const bf16x8 k = *lds_at<bf16x8>(k_at[ks] + (block & 1) * kBlockBytes + t * 32 * 256);
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[ks], s[t], 0, 0, 0);
+                }
+            }
+        };
+        // 16 keys from 16 s and 32 dims from 32 d of the values, transposed: keys 4 half .. + 3, then 8 + 4 half .. + 3, of the lane's dim
+        auto values = [&](int block, int s, int d) {
+            auto* p = lds_at<s16x4>(v_at[d] + (block & 1) * kBlockBytes + s * 16 * 256);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(v_at[d] + (block & 1) * kBlockBytes + s * 16 * 256 + 8 * 256));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+
+        Softmax st;
+        st.m = -INFINITY;
+        st.l = 0.f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) st.o[d][j] = 0.f;
+
+        int pages_next[2], pages_now[2];
+        uint4 kw[2], vw[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            pages_now[e] = page_at(first, e);
+            pages_next[e] = page_at(first + 1, e);
+        }
+        load(a.c.K, first, pages_now, kw);
+        load(a.c.V, first, pages_now, vw);
+        workgroup_sync();                                  // (the item before is done with LDS)
+        store_k(first, pages_now, kw);
+        store_v(first, vw);
+        load(a.c.K, first + 1, pages_next, kw);
+        load(a.c.V, first + 1, pages_next, vw);
+        workgroup_sync();
+
+        for (int t = first; t < last; ++t) {
+            int pages_far[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) pages_far[e] = page_at(t + 2, e);
+            if (active && t * kKeys <= pos_max) {
+                f32x16 s[2];
+                scores(t, s);
+                const unsigned long long valid = *reinterpret_cast<const unsigned long long*>(lds_valid[t & 1]);
+                const uint32_t valid_lo = __builtin_amdgcn_readfirstlane((uint32_t)valid), valid_hi = __builtin_amdgcn_readfirstlane((uint32_t)(valid >> 32));
+                const bool masked = (valid_lo & valid_hi) != 0xffffffffu || t * kKeys + kKeys - 1 > pos_min || (a.window && t * kKeys <= pos_max - a.window);
+                if (masked) {
+                    const int upto = position - t * kKeys, from = a.window ? upto - a.window : -1;      // keys (from, upto] of the block
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt) {
+                        const uint32_t in = (tt ? valid_hi : valid_lo) >> (4 * half);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const int k = 32 * tt + 8 * (j >> 2) + (j & 3) + 4 * half;
+                            const bool seen = (in >> (8 * (j >> 2) + (j & 3)) & 1) && k <= upto && k > from;
+                            s[tt][j] = seen ? s[tt][j] : -INFINITY;
+                        }
+                    }
+                }
+                float mx = s[0][0];
+#pragma unroll
+                for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s[0][j]);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[1][j]);
+                mx = over_halves_max(mx) * scale;
+                // The maximum in use may be up to 2^8 behind: sums in fp32 and products of bf16 have room for it, and it is soon never moved.
+                if (__any(mx > st.m + 8.f)) {
+                    const float m = fmaxf(st.m, mx), f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
+                    st.m = m;
+                    st.l *= f;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) st.o[d][j] *= f;
+                }
+                const float m = st.m == -INFINITY ? 0.f : st.m;
+                bf16x8 p[4];
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(s[tt][j], scale, -m));
+                        st.l += e;
+                        p[2 * tt + (j >> 3)][j & 7] = (__bf16)e;
+                    }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                        st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(t, k, d)), p[k], st.o[d], 0, 0, 0);
+                // Values that are not finite have been taken out of an edge's block, lest they meet the zero of a row that does not see them: they are
+                // added to the rows that do.
+                if (edge(t)) {
+                    const unsigned long long flags = *reinterpret_cast<const unsigned long long*>(lds_odd[t & 1]);
+                    unsigned long long odd = (unsigned long long)__builtin_amdgcn_readfirstlane((uint32_t)(flags >> 32)) << 32 | __builtin_amdgcn_readfirstlane((uint32_t)flags);
+                    for (; odd; odd &= odd - 1) {
+                        const int key = t * kKeys + __ffsll((long long)odd) - 1;
+                        const int page = __builtin_amdgcn_readfirstlane(page_of(entries, a.c.table_stride, a.c.n_pages, a.c.page_shift, key));
+                        const bool sees = key <= position && !(a.window && key <= position - a.window);
+                        const uint2* from = reinterpret_cast<const uint2*>(a.c.V + row_of(page, h, a.c.n_kv, a.c.page_shift, key) * kHeadDim);
+#pragma unroll
+                        for (int d = 0; d < 4; ++d)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint2 w = from[8 * d + 2 * j + half];
+                                const uint32_t u[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (sees && (u[e] & 0x7f800000u) == 0x7f800000u) st.o[d][4 * j + e] += __uint_as_float(u[e]);
+                            }
+                    }
+                }
+            }
+            store_k(t + 1, pages_next, kw);
+            store_v(t + 1, vw);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) pages_next[e] = pages_far[e];
+            load(a.c.K, t + 2, pages_next, kw);
+            load(a.c.V, t + 2, pages_next, vw);
+            workgroup_sync();
+        }
+
+        const float l = over_halves_sum(st.l);
+        if (whole) store_rows(a, st, l, it.rows.q0 + i, head, wave * 32 + (lane & 31) < tile_rows);
+        else store_part(parts + (long long)(2 * share + (x > share * line.share ? 1 : 0)) * kPartFloats, st, l);
+        x += last - first;
+    }
+}
+
+// One workgroup a cut and 32 rows: the parts of an item that begins in this share and ends in another.
+__global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a, Tiling tl, const float* parts)
+{
+    const Line line = line_of(a, tl);
+    const int share = blockIdx.x >> 3, wave = blockIdx.x & 7, lane = threadIdx.x;
+    if (share + 1 >= line.used) return;
+    const long long cut = (share + 1) * line.share;
+    const int h = (int)((cut - 1) / line.of_head);
+    Item it;
+    const long long head_first = (long long)h * line.of_head;
+    walk<true>(a, tl, (uint32_t)(cut - 1 - head_first), &it);
+    const long long x0 = head_first + it.before, x1 = x0 + (it.b1 - it.b0);
+    if (x0 < share * line.share || x1 <= cut) return;
+    const int tile_rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * tl.group;
+    if (wave * 32 >= tile_rows) return;
+    const Parts in = parts_of(x0, x1, line.share);
+    auto part = [&](long long g) { return parts + (2 * g + slot_of(x0, g, line.share)) * kPartFloats; };
+    Softmax st;
+    st.m = -INFINITY;
+    for (long long g = in.first; g <= in.last; ++g) st.m = fmaxf(st.m, part(g)[kRows * kHeadDim + wave * 32 + (lane & 31)]);
+    float l = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) st.o[d][j] = 0.f;
+    for (long long g = in.first; g <= in.last; ++g) {
+        const float* p = part(g);
+        const float m = p[kRows * kHeadDim + wave * 32 + (lane & 31)];
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - st.m);
+        l = fmaf(p[kRows * kHeadDim + kRows + wave * 32 + (lane & 31)], f, l);
+        const f32x4* o = reinterpret_cast<const f32x4*>(p) + wave * 16 * 64 + lane;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 w = o[(4 * d + j) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.o[d][4 * j + e] = m == -INFINITY ? st.o[d][4 * j + e] : fmaf(w[e], f, st.o[d][4 * j + e]);
+            }
+    }
+    const int r = min(wave * 32 + (lane & 31), tile_rows - 1);
+    store_rows(a, st, l, it.rows.q0 + it.tile * tl.tokens + r / tl.group, h * tl.group + r % tl.group, wave * 32 + (lane & 31) < tile_rows);
+}
+
+Tiling chunk_tiling(int group, int over)
+{
+    Tiling t;
+    t.group = group;
+    t.tokens = kRows / group;
+    t.over = over;
+    t.most = 0x7fffffff;
+    t.unit = kKeys;
+    t.least = 4;
+    t.workgroups = kWorkgroups;
+    return t;
+}
+
+}  // namespace
+
+size_t paged_chunk_floats() { return (size_t)2 * kWorkgroups * kPartFloats; }
+
+hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* parts, hipStream_t s)
+{
+    const Tiling tl = chunk_tiling(a.n_q_heads / a.c.n_kv, over);
+    hipLaunchKernelGGL(paged_chunk_kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(8 * (kWorkgroups - 1)), dim3(64), 0, s, a, tl, (const float*)parts);
+    return hipGetLastError();
+}
+
+}  // namespace mp

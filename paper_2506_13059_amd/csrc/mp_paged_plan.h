@@ -1,0 +1,140 @@
+// How attention over a paged cache is shared out: device code of mp_paged_chunk.hip and mp_paged_token.hip.
+//
+// A sequence's query rows of one KV head are its new tokens times the G heads of the group, token after token.  An item is a tile of such rows
+// with the blocks of keys that some of them attend.  All items' blocks, head after head, sequence after sequence, are one line that is cut into equal
+// shares, a workgroup each: lengths are known on the device only, and one long sequence among short ones, or few rows over many keys,
+// come out even.  An item within a share is finished there; one that is cut leaves its parts (maximum, sum and weighted values, in fp32) in the
+// workspace for the launch behind.
+#pragma once
+#include "mp_device.h"
+#include "mp_paged.h"
+
+namespace mp {
+
+namespace {
+
+// A sequence is an item's if it has more than `over` and at most `most` rows.
+struct Tiling {
+    int group;                // G
+    int tokens;               // of a tile
+    int over, most;
+    int unit;                 // keys of a block
+    int least;                // blocks of a share, at least
+    int workgroups;
+};
+
+struct SequenceRows {
+    int q0, n, base;          // first token, tokens, position of the first
+};
+
+__device__ __forceinline__ SequenceRows rows_of_sequence(const PagedAttention& a, int b)
+{
+    const int s0 = a.c.q_start[b], s1 = a.c.q_start[b + 1];
+    SequenceRows r;
+    r.q0 = min(max(s0, 0), a.n_tokens);
+    r.n = min(min(max(s1, r.q0), a.n_tokens) - r.q0, a.max_new);
+    r.base = a.c.kv_len[b] - (s1 - s0);
+    return r;
+}
+
+struct Item {
+    int b, tile;
+    SequenceRows rows;
+    int b0, b1;               // its blocks
+    uint32_t before;          // blocks of the items before it (of one head)
+};
+
+__device__ __forceinline__ int room_of(const PagedAttention& a) { return a.c.table_stride << a.c.page_shift; }
+
+__device__ __forceinline__ void blocks_of_tile(const PagedAttention& a, const Tiling& tl, const SequenceRows& r, int tile, int* b0, int* b1)
+{
+    const int i0 = tile * tl.tokens;
+    blocks_of(r.base, i0, min(r.n, i0 + tl.tokens) - 1, a.window, room_of(a), tl.unit, b0, b1);
+}
+
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// Blocks of one head's items in all; kFind: up to the item that block x of the line lies in, which goes to *found.  One wave, 64 sequences (or,
+// where some have several tiles, 64 tiles) at a time.
+template <bool kFind>
+__device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, uint32_t x, Item* found)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t sum = 0;
+    for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
+        SequenceRows r{0, 0, 0};
+        if (s0 + lane < a.c.n_seqs) r = rows_of_sequence(a, s0 + lane);
+        const long long rows = (long long)r.n * tl.group;
+        const int tiles = rows > tl.over && rows <= tl.most ? (r.n + tl.tokens - 1) / tl.tokens : 0;
+        const bool several = __any(tiles > 1);
+        const int upto = several ? (int)wave_incl_scan_u32((uint32_t)tiles) : 0;
+        const int all = several ? lane_value(upto, 63) : 64;
+        for (int c = 0; c < all; c += 64) {
+            int k = lane, tile = 0;
+            SequenceRows m = r;
+            bool there = tiles > 0;
+            if (several) {
+                k = 0;
+#pragma unroll
+                for (int step = 32; step; step >>= 1)
+                    if (__shfl(upto, k + step - 1, 64) <= c + lane) k += step;
+                tile = c + lane - (__shfl(upto, k, 64) - __shfl(tiles, k, 64));
+                m.q0 = __shfl(r.q0, k, 64);
+                m.n = __shfl(r.n, k, 64);
+                m.base = __shfl(r.base, k, 64);
+                there = c + lane < all;
+            }
+            int b0 = 0, b1 = 0;
+            if (there) blocks_of_tile(a, tl, m, tile, &b0, &b1);
+            const uint32_t incl = wave_incl_scan_u32((uint32_t)(b1 - b0));
+            if constexpr (kFind) {
+                const unsigned long long past = __ballot(sum + incl > x);
+                if (past) {
+                    const int at = __ffsll((long long)past) - 1;
+                    found->b = s0 + lane_value(k, at);
+                    found->tile = lane_value(tile, at);
+                    found->rows.q0 = lane_value(m.q0, at);
+                    found->rows.n = lane_value(m.n, at);
+                    found->rows.base = lane_value(m.base, at);
+                    found->b0 = lane_value(b0, at);
+                    found->b1 = lane_value(b1, at);
+                    found->before = sum + (uint32_t)lane_value((int)incl, at) - (uint32_t)(found->b1 - found->b0);
+                    return sum;
+                }
+            }
+            sum += (uint32_t)lane_value((int)incl, 63);
+        }
+    }
+    return sum;
+}
+
+// The line and its shares.  Neighbouring shares go to workgroups of one XCD: they mostly work on one head, whose keys its L2 then holds once.
+struct Line {
+    uint32_t of_head;
+    long long all, share;
+    int used;                 // workgroups with a share
+};
+__device__ __forceinline__ Line line_of(const PagedAttention& a, const Tiling& tl)
+{
+    Line l;
+    l.of_head = walk<false>(a, tl, 0, nullptr);
+    l.all = (long long)l.of_head * a.c.n_kv;
+    l.share = max((l.all + tl.workgroups - 1) / tl.workgroups, (long long)tl.least);
+    l.used = (int)((l.all + l.share - 1) / l.share);
+    return l;
+}
+// The share of a workgroup (of tl.workgroups), or -1.
+__device__ __forceinline__ int share_of(const Line& l, int block)
+{
+    const int of_xcd = (l.used + 7) >> 3, i = block >> 3, s = (block & 7) * of_xcd + i;
+    return i < of_xcd && s < l.used ? s : -1;
+}
+
+// Query row r (of an item's tile): its token and head.
+struct RowAt {
+    int token, head;          // token of the call, query head
+    int position;
+};
+
+}  // namespace
+}  // namespace mp
