@@ -48,8 +48,11 @@ struct PagedAttention {
     float* partials;
 };
 size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_seqs, int max_new);
+constexpr int kPagedTokenRows = 16;      // query rows a KV head that the kernel for single tokens takes
+size_t paged_token_floats();
+hipError_t launch_paged_tokens(const PagedAttention& a, float* room, hipStream_t s);                // sequences of up to that many
 size_t paged_chunk_floats();
-hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* parts, hipStream_t s);     // sequences of more than `over` query rows a head
+hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s);     // sequences of more than `over` query rows a head
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s);
 
 // The sequence of token t: the last one that starts at or before it (sequences without new tokens start where the next one does), or -1

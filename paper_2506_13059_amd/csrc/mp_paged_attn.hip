@@ -8,15 +8,39 @@
 
 namespace mp {
 
+namespace {
+
+// Which kernels a call runs: those for single tokens take sequences of few query rows, those for chunks the others, or all where no sequence need
+// have few (there is one, or the call's tokens are as many as its sequences can have).
+struct Kernels {
+    bool tokens, chunks;
+};
+Kernels kernels_of(int n_tokens, int group, int n_seqs, int max_new)
+{
+    if ((long long)max_new * group <= kPagedTokenRows) return Kernels{true, false};
+    return Kernels{n_seqs > 1 && (long long)n_seqs * max_new > n_tokens, true};
+}
+
+}  // namespace
+
 size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_seqs, int max_new)
 {
-    return n_tokens > 0 ? paged_chunk_floats() : 0;
+    if (n_tokens <= 0 || n_seqs <= 0) return 0;
+    const Kernels k = kernels_of(n_tokens, n_q_heads / n_kv_heads, n_seqs, max_new);
+    return (k.tokens ? paged_token_floats() : 0) + (k.chunks ? paged_chunk_floats() : 0);
 }
 
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s)
 {
     if (a.n_tokens <= 0 || a.c.n_seqs <= 0) return hipSuccess;
-    return launch_paged_chunks(a, 0, a.partials, s);
+    const Kernels k = kernels_of(a.n_tokens, a.n_q_heads / a.c.n_kv, a.c.n_seqs, a.max_new);
+    float* room = a.partials;
+    if (k.tokens) {
+        const hipError_t e = launch_paged_tokens(a, room, s);
+        if (e != hipSuccess) return e;
+        room += paged_token_floats();
+    }
+    return k.chunks ? launch_paged_chunks(a, k.tokens ? kPagedTokenRows : 0, room, s) : hipSuccess;
 }
 
 }  // namespace mp

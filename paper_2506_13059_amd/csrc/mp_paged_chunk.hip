@@ -88,7 +88,7 @@ __device__ __forceinline__ void store_part(float* part, const Softmax& st, float
     }
 }
 
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts)
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
 {
     __shared__ __align__(256) unsigned char lds_k[2][kBlockBytes];
     __shared__ __align__(256) unsigned char lds_v[2][kBlockBytes];
@@ -97,7 +97,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
     const Line line = line_of(a, tl);
     const int share = share_of(line, blockIdx.x);
-    if (share < 0) return;
+    if (share >= line.used) {
+        if (threadIdx.x == 0) cuts[share].parts = 0;
+        return;
+    }
     const float scale = a.scale_log2e;
     const int G = tl.group;
 
@@ -118,6 +121,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
 
     long long x = share * line.share;
     const long long x_end = min(x + line.share, line.all);
+    Cut cut{};
     while (x < x_end) {
         const int h = (int)(x / line.of_head);
         Item it;
@@ -335,41 +339,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
 
         const float l = over_halves_sum(st.l);
         if (whole) store_rows(a, st, l, it.rows.q0 + i, head, wave * 32 + (lane & 31) < tile_rows);
-        else store_part(parts + (long long)(2 * share + (x > share * line.share ? 1 : 0)) * kPartFloats, st, l);
+        else {
+            store_part(parts + (2ll * share + (x > share * line.share ? 1 : 0)) * kPartFloats, st, l);
+            if (last < it.b1) cut = cut_of(it, tl, line, share, h);
+        }
         x += last - first;
     }
+    if (threadIdx.x == 0) cuts[share] = cut;
 }
 
-// One workgroup a cut and 32 rows: the parts of an item that begins in this share and ends in another.
-__global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a, Tiling tl, const float* parts)
+// One wave a cut and 32 rows.
+__global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a, int group, const float* parts, const Cut* cuts)
 {
-    const Line line = line_of(a, tl);
     const int share = blockIdx.x >> 3, wave = blockIdx.x & 7, lane = threadIdx.x;
-    if (share + 1 >= line.used) return;
-    const long long cut = (share + 1) * line.share;
-    const int h = (int)((cut - 1) / line.of_head);
-    Item it;
-    const long long head_first = (long long)h * line.of_head;
-    walk<true>(a, tl, (uint32_t)(cut - 1 - head_first), &it);
-    const long long x0 = head_first + it.before, x1 = x0 + (it.b1 - it.b0);
-    if (x0 < share * line.share || x1 <= cut) return;
-    const int tile_rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * tl.group;
-    if (wave * 32 >= tile_rows) return;
-    const Parts in = parts_of(x0, x1, line.share);
-    auto part = [&](long long g) { return parts + (2 * g + slot_of(x0, g, line.share)) * kPartFloats; };
+    const Cut c = cuts[share];
+    if (c.parts == 0 || wave * 32 >= c.rows) return;
+    auto part = [&](int g) { return parts + (2ll * (share + g) + (g == 0 ? c.slot : 0)) * kPartFloats; };
+    const int at_m = kRows * kHeadDim + wave * 32 + (lane & 31);
     Softmax st;
     st.m = -INFINITY;
-    for (long long g = in.first; g <= in.last; ++g) st.m = fmaxf(st.m, part(g)[kRows * kHeadDim + wave * 32 + (lane & 31)]);
+    for (int g = 0; g < c.parts; ++g) st.m = fmaxf(st.m, part(g)[at_m]);
     float l = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int j = 0; j < 16; ++j) st.o[d][j] = 0.f;
-    for (long long g = in.first; g <= in.last; ++g) {
+    for (int g = 0; g < c.parts; ++g) {
         const float* p = part(g);
-        const float m = p[kRows * kHeadDim + wave * 32 + (lane & 31)];
+        const float m = p[at_m];
         const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - st.m);
-        l = fmaf(p[kRows * kHeadDim + kRows + wave * 32 + (lane & 31)], f, l);
+        l = fmaf(p[at_m + kRows], f, l);
         const f32x4* o = reinterpret_cast<const f32x4*>(p) + wave * 16 * 64 + lane;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
@@ -377,11 +376,11 @@ __global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a,
             for (int j = 0; j < 4; ++j) {
                 const f32x4 w = o[(4 * d + j) * 64];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) st.o[d][4 * j + e] = m == -INFINITY ? st.o[d][4 * j + e] : fmaf(w[e], f, st.o[d][4 * j + e]);
+                for (int e = 0; e < 4; ++e) st.o[d][4 * j + e] = fmaf(w[e], f, st.o[d][4 * j + e]);
             }
     }
-    const int r = min(wave * 32 + (lane & 31), tile_rows - 1);
-    store_rows(a, st, l, it.rows.q0 + it.tile * tl.tokens + r / tl.group, h * tl.group + r % tl.group, wave * 32 + (lane & 31) < tile_rows);
+    const int r = min(wave * 32 + (lane & 31), c.rows - 1);
+    store_rows(a, st, l, c.q0 + r / group, c.head * group + r % group, wave * 32 + (lane & 31) < c.rows);
 }
 
 Tiling chunk_tiling(int group, int over)
@@ -397,17 +396,21 @@ Tiling chunk_tiling(int group, int over)
     return t;
 }
 
+constexpr size_t kCutFloats = sizeof(Cut) / sizeof(float) * kWorkgroups;
+
 }  // namespace
 
-size_t paged_chunk_floats() { return (size_t)2 * kWorkgroups * kPartFloats; }
+size_t paged_chunk_floats() { return (size_t)2 * kWorkgroups * kPartFloats + kCutFloats; }
 
-hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* parts, hipStream_t s)
+hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s)
 {
     const Tiling tl = chunk_tiling(a.n_q_heads / a.c.n_kv, over);
-    hipLaunchKernelGGL(paged_chunk_kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts);
+    Cut* cuts = reinterpret_cast<Cut*>(room);
+    float* parts = room + kCutFloats;
+    hipLaunchKernelGGL(paged_chunk_kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(8 * (kWorkgroups - 1)), dim3(64), 0, s, a, tl, (const float*)parts);
+    hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(8 * kWorkgroups), dim3(64), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
     return hipGetLastError();
 }
 

@@ -123,18 +123,34 @@ __device__ __forceinline__ Line line_of(const PagedAttention& a, const Tiling& t
     l.used = (int)((l.all + l.share - 1) / l.share);
     return l;
 }
-// The share of a workgroup (of tl.workgroups), or -1.
+// The share of a workgroup (of tl.workgroups); those from l.used on are empty.
 __device__ __forceinline__ int share_of(const Line& l, int block)
 {
-    const int of_xcd = (l.used + 7) >> 3, i = block >> 3, s = (block & 7) * of_xcd + i;
-    return i < of_xcd && s < l.used ? s : -1;
+    const int of_xcd = (l.used + 7) >> 3, xcd = block & 7, i = block >> 3;
+    if (i < of_xcd) return xcd * of_xcd + i;
+    return 8 * of_xcd + (i - of_xcd) * 8 + xcd;
 }
 
-// Query row r (of an item's tile): its token and head.
-struct RowAt {
-    int token, head;          // token of the call, query head
-    int position;
+// An item that begins in a workgroup's share and ends in another one's, for the launch that puts its parts together: a line for each
+// workgroup, written by it (parts == 0: none).
+struct Cut {
+    int parts;                // workgroups with a part of it, this one first
+    int slot;                 // of this workgroup's part; the others' are their first
+    int q0, rows, head;       // first token, query rows, KV head
+    int unused[3];
 };
+__device__ __forceinline__ Cut cut_of(const Item& it, const Tiling& tl, const Line& line, int share, int h)
+{
+    const long long x0 = (long long)h * line.of_head + it.before;
+    const Parts p = parts_of(x0, x0 + (it.b1 - it.b0), line.share);
+    Cut c{};
+    c.parts = p.first == share ? (int)(p.last - p.first) + 1 : 0;
+    c.slot = slot_of(x0, share, line.share);
+    c.q0 = it.rows.q0 + it.tile * tl.tokens;
+    c.rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * tl.group;
+    c.head = h;
+    return c;
+}
 
 }  // namespace
 }  // namespace mp
