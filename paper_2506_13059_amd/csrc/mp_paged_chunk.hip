@@ -54,6 +54,9 @@ __device__ __forceinline__ void workgroup_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The lowest n of 64 bits.
+__device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
+
 // The rows of a finished item.
 __device__ __forceinline__ void store_rows(const PagedAttention& a, const Softmax& st, float l, int token, int head, bool there)
 {
@@ -88,7 +91,7 @@ __device__ __forceinline__ void store_part(float* part, const Softmax& st, float
     }
 }
 
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
 {
     __shared__ __align__(256) unsigned char lds_k[2][kBlockBytes];
     __shared__ __align__(256) unsigned char lds_v[2][kBlockBytes];
@@ -104,9 +107,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
     const float scale = a.scale_log2e;
     const int G = tl.group;
 
-    // LDS addresses: of the lane's row in the first 32 keys, chunk 2 ks + half; of its place in the first 16 values, dims 32 d
-    uint32_t k_at[8], v_at[4];
+    // LDS addresses: of the lane's row in the first 32 keys, chunk 2 ks + half; of its place in the first 16 values, dims 32 d; and of what it loads
+    uint32_t k_at[8], v_at[4], k_to, v_to;
     {
+        const int g = lane >> 4, c = lane & 15;
+        k_to = lds_offset(lds_k) + (8 * wave + g) * 256 + ((c ^ (8 * (wave & 1) + g)) << 4);
+        v_to = lds_offset(lds_v) + (8 * wave + g) * 256 + ((c ^ (g << 2)) << 4);
         const int row = lane & 31, v_row = 4 * half + ((lane & 15) >> 2);
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) k_at[ks] = lds_offset(lds_k) + row * 256 + (((2 * ks + half) ^ (row & 15)) << 4);
@@ -119,6 +125,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
         for (int d = 0; d < 4; ++d) asm volatile("" : "+v"(v_at[d]));
     }
 
+#ifdef PRIO
+    if (wave < 4) __builtin_amdgcn_s_setprio(PRIO);
+#endif
     long long x = share * line.share;
     const long long x_end = min(x + line.share, line.all);
     Cut cut{};
@@ -145,78 +154,119 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
         }
 
         // Loading: rows 8 wave + 4 e + lane / 16 of a block, chunk lane % 16 of 16 bytes.  In LDS chunk j of row k lies at j ^ k % 16 (keys) or j ^ 4 (k % 4)
-        // (values): what the lanes of a read touch together lies in different banks.
+        // (values): what the lanes of a read touch together lies in different banks.  Pages of eight rows or more hold all that a wave loads of a
+        // block, so its address is a scalar.
         const int32_t* entries = a.c.table + (long long)it.b * a.c.table_stride;
         const int chunk = lane & 15;
         const int end = min(it.rows.base + it.rows.n, room_of(a));       // keys of the sequence
-        auto page_at = [&](int block, int e) {
-            const int key = block * kKeys + 8 * wave + 4 * e + (lane >> 4);
-            return key < end ? page_of(entries, a.c.table_stride, a.c.n_pages, a.c.page_shift, key) : -1;
+        const bool one_page = a.c.page_shift >= 3;
+        // (entries are looked at a block after they were asked for: looked at at once, they made a wave wait for all loads before them)
+        auto entry_at = [&](int block, int (&entry)[2]) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (e == 1 && one_page) break;
+                const int key = block * kKeys + 8 * wave + (one_page ? 0 : 4 * e + (lane >> 4));
+                entry[e] = entries[min(key, end - 1) >> a.c.page_shift];
+            }
         };
-        auto offset_at = [&](int block, int e, int page) {
-            return row_of(max(page, 0), h, a.c.n_kv, a.c.page_shift, block * kKeys + 8 * wave + 4 * e + (lane >> 4)) * 16 + chunk;
-        };
+        auto held = [&](int entry, int key) { return key < end && (uint32_t)entry < (uint32_t)a.c.n_pages; };
         const uint4 zero = make_uint4(0, 0, 0, 0);
-        auto load = [&](const uint16_t* base, int block, const int (&page)[2], uint4 (&w)[2]) {
+        // One block's rows of this wave; what is not there keeps what the registers held.
+        auto load = [&](int block, const int (&entry)[2], uint4 (&kw)[2], uint4 (&vw)[2]) {
+            const int key = block * kKeys + 8 * wave;
+            if (one_page) {
+                const int page = __builtin_amdgcn_readfirstlane(entry[0]);
+                if (held(page, key)) {
+                    const long long at = row_of(page, h, a.c.n_kv, a.c.page_shift, key) * 16;
+                    const uint4 *k = reinterpret_cast<const uint4*>(a.c.K) + at, *v = reinterpret_cast<const uint4*>(a.c.V) + at;
+                    kw[0] = k[(uint32_t)lane];
+                    kw[1] = k[(uint32_t)lane + 64];
+                    vw[0] = v[(uint32_t)lane];
+                    vw[1] = v[(uint32_t)lane + 64];
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                w[e] = zero;
-                if (page[e] >= 0) w[e] = reinterpret_cast<const uint4*>(base)[offset_at(block, e, page[e])];
+                for (int e = 0; e < 2; ++e) {
+                    const int row_key = key + 4 * e + (lane >> 4);
+                    if (held(entry[e], row_key)) {
+                        const long long at = row_of(entry[e], h, a.c.n_kv, a.c.page_shift, row_key) * 16 + chunk;
+                        kw[e] = reinterpret_cast<const uint4*>(a.c.K)[at];
+                        vw[e] = reinterpret_cast<const uint4*>(a.c.V)[at];
+                    }
+                }
             }
-        };
-        auto store_k = [&](int block, const int (&page)[2], const uint4 (&w)[2]) {
-            uint32_t bits = 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int row = 8 * wave + 4 * e + (lane >> 4);
-                *reinterpret_cast<uint4*>(&lds_k[block & 1][row * 256 + ((chunk ^ (row & 15)) << 4)]) = w[e];
-                const unsigned long long in = __ballot(page[e] >= 0);
-                bits |= ((uint32_t)(in & 1) | (uint32_t)(in >> 15 & 2) | (uint32_t)(in >> 30 & 4) | (uint32_t)(in >> 45 & 8)) << (4 * e);
-            }
-            if (lane == 0) lds_valid[block & 1][wave] = (unsigned char)bits;
         };
         // a block in which some row of the item sees a key that another one does not
         auto edge = [&](int block) {
             return block * kKeys + kKeys - 1 > it.rows.base + it.tile * tl.tokens ||
                    (a.window && block * kKeys <= it.rows.base + min(it.rows.n, (it.tile + 1) * tl.tokens) - 1 - a.window);
         };
-        auto store_v = [&](int block, uint4 (&w)[2]) {
-            uint32_t bits = 0;
+        auto store = [&](int block, const int (&entry)[2], uint4 (&kw)[2], uint4 (&vw)[2]) {
+            uint32_t bits = 0, odd = 0;
+            if (one_page) {
+                const int n = end - (block * kKeys + 8 * wave);
+                if ((uint32_t)__builtin_amdgcn_readfirstlane(entry[0]) < (uint32_t)a.c.n_pages) bits = n >= 8 ? 255u : n > 0 ? (1u << n) - 1u : 0u;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const unsigned long long in = __ballot(held(entry[e], block * kKeys + 8 * wave + 4 * e + (lane >> 4)));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) bits |= (uint32_t)(in >> (16 * k) & 1) << (4 * e + k);
+                }
+            }
+            if (bits != 255u) {              // (rows without a key are zero: a probability of zero meets them)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (!(bits >> (4 * e + (lane >> 4)) & 1)) vw[e] = zero;
+            }
             if (edge(block)) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    uint32_t u[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
-                    bool odd = false;
+                    uint32_t u[4] = {vw[e].x, vw[e].y, vw[e].z, vw[e].w};
+                    bool off_range = false;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const bool lo = (u[k] & 0x7f80u) == 0x7f80u, hi = (u[k] & 0x7f800000u) == 0x7f800000u;
-                        odd |= lo | hi;
+                        off_range |= lo | hi;
                         u[k] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
                     }
-                    w[e] = make_uint4(u[0], u[1], u[2], u[3]);
-                    const unsigned long long in = __ballot(odd);
+                    vw[e] = make_uint4(u[0], u[1], u[2], u[3]);
+                    const unsigned long long in = __ballot(off_range);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) bits |= (uint32_t)((in >> (16 * k) & 0xffff) != 0) << (4 * e + k);
+                    for (int k = 0; k < 4; ++k) odd |= (uint32_t)((in >> (16 * k) & 0xffff) != 0) << (4 * e + k);
                 }
             }
-            if (lane == 0) lds_odd[block & 1][wave] = (unsigned char)bits;
+            if (lane == 0) {
+                lds_valid[block & 1][wave] = (unsigned char)bits;
+                lds_odd[block & 1][wave] = (unsigned char)odd;
+            }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int row = 8 * wave + 4 * e + (lane >> 4);
-                *reinterpret_cast<uint4*>(&lds_v[block & 1][row * 256 + ((chunk ^ ((row & 3) << 2)) << 4)]) = w[e];
+                *lds_at<u32x4>((e ? k_to ^ 64u : k_to) + (block & 1) * kBlockBytes + e * 1024) = u32x4{kw[e].x, kw[e].y, kw[e].z, kw[e].w};
+                *lds_at<u32x4>(v_to + (block & 1) * kBlockBytes + e * 1024) = u32x4{vw[e].x, vw[e].y, vw[e].z, vw[e].w};
             }
         };
 
+        // (reads kAhead ahead of the products that take them: left alone, the compiler has each product wait for a read of its own)
         auto scores = [&](int block, f32x16 (&s)[2]) {
+#ifndef KA
+#define KA 4
+#endif
+            constexpr int kAhead = KA;
+            bf16x8 k[kAhead];
+            auto read = [&](int i) { k[i % kAhead] = *lds_at<bf16x8>(k_at[i >> 1] + (block & 1) * kBlockBytes + (i & 1) * 32 * 256); };
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    const bf16x8 k = *lds_at<bf16x8>(k_at[ks] + (block & 1) * kBlockBytes + t * 32 * 256);
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[ks], s[t], 0, 0, 0);
-                }
+            for (int i = 0; i < kAhead; ++i) read(i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i % kAhead], q[i >> 1], s[i & 1], 0, 0, 0);
+                if (i + kAhead < 16) read(i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
         // 16 keys from 16 s and 32 dims from 32 d of the values, transposed: keys 4 half .. + 3, then 8 + 4 half .. + 3, of the lane's dim
@@ -235,26 +285,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
 #pragma unroll
             for (int j = 0; j < 16; ++j) st.o[d][j] = 0.f;
 
-        int pages_next[2], pages_now[2];
-        uint4 kw[2], vw[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            pages_now[e] = page_at(first, e);
-            pages_next[e] = page_at(first + 1, e);
-        }
-        load(a.c.K, first, pages_now, kw);
-        load(a.c.V, first, pages_now, vw);
-        workgroup_sync();                                  // (the item before is done with LDS)
-        store_k(first, pages_now, kw);
-        store_v(first, vw);
-        load(a.c.K, first + 1, pages_next, kw);
-        load(a.c.V, first + 1, pages_next, vw);
-        workgroup_sync();
-
-        for (int t = first; t < last; ++t) {
-            int pages_far[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) pages_far[e] = page_at(t + 2, e);
+        uint4 kw[2] = {zero, zero}, vw[2] = {zero, zero};
+        if (end > 0) {
+            int now[2], next[2];
+            entry_at(first, now);
+            entry_at(first + 1, next);
+            load(first, now, kw, vw);
+            workgroup_sync();                              // (the item before is done with LDS)
+            store(first, now, kw, vw);
+            load(first + 1, next, kw, vw);
+            workgroup_sync();
+            for (int t = first; t < last; ++t) {
+            int far[2];
+            entry_at(t + 2, far);
             if (active && t * kKeys <= pos_max) {
                 f32x16 s[2];
                 scores(t, s);
@@ -262,16 +305,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
                 const uint32_t valid_lo = __builtin_amdgcn_readfirstlane((uint32_t)valid), valid_hi = __builtin_amdgcn_readfirstlane((uint32_t)(valid >> 32));
                 const bool masked = (valid_lo & valid_hi) != 0xffffffffu || t * kKeys + kKeys - 1 > pos_min || (a.window && t * kKeys <= pos_max - a.window);
                 if (masked) {
-                    const int upto = position - t * kKeys, from = a.window ? upto - a.window : -1;      // keys (from, upto] of the block
+                    // keys (from, upto] of the block, those that are there; bit k of `see` for key 4 half + k
+                    const int upto = position - t * kKeys, from = a.window ? upto - a.window : -1;
+                    const unsigned long long see = (valid & below(upto + 1) & ~below(from + 1)) >> (4 * half);
 #pragma unroll
                     for (int tt = 0; tt < 2; ++tt) {
-                        const uint32_t in = (tt ? valid_hi : valid_lo) >> (4 * half);
+                        const uint32_t in = (uint32_t)(see >> (32 * tt));
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const int k = 32 * tt + 8 * (j >> 2) + (j & 3) + 4 * half;
-                            const bool seen = (in >> (8 * (j >> 2) + (j & 3)) & 1) && k <= upto && k > from;
-                            s[tt][j] = seen ? s[tt][j] : -INFINITY;
-                        }
+                        for (int j = 0; j < 16; ++j) s[tt][j] = in & (1u << (8 * (j >> 2) + (j & 3))) ? s[tt][j] : -INFINITY;
                     }
                 }
                 float mx = s[0][0];
@@ -291,20 +332,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
                         for (int j = 0; j < 16; ++j) st.o[d][j] *= f;
                 }
                 const float m = st.m == -INFINITY ? 0.f : st.m;
+                // Probabilities of 16 keys at a time, two elements behind each product of the 16 keys before; values are read two products ahead.
                 bf16x8 p[4];
+                auto probabilities = [&](int k, int e) {
 #pragma unroll
-                for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(s[tt][j], scale, -m));
-                        st.l += e;
-                        p[2 * tt + (j >> 3)][j & 7] = (__bf16)e;
+                    for (int j = e; j < e + 2; ++j) {
+                        const float x = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][8 * (k & 1) + j], scale, -m));
+                        st.l += x;
+                        p[k][j] = (__bf16)x;
                     }
+                };
+#ifndef VA
+#define VA 2
+#endif
+                constexpr int kAhead = VA;
+                s16x8 v[kAhead];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int i = 0; i < kAhead; ++i) v[i] = values(t, 0, i);
 #pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                        st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(t, k, d)), p[k], st.o[d], 0, 0, 0);
+                for (int e = 0; e < 8; e += 2) probabilities(0, e);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[i % kAhead]), p[i >> 2], st.o[i & 3], 0, 0, 0);
+                    if (i + kAhead < 16) v[i % kAhead] = values(t, (i + kAhead) >> 2, (i + kAhead) & 3);
+                    if (i < 12) probabilities((i >> 2) + 1, 2 * (i & 3));
+#ifndef NOSB
+                    __builtin_amdgcn_sched_barrier(0);
+#endif
+                }
                 // Values that are not finite have been taken out of an edge's block, lest they meet the zero of a row that does not see them: they are
                 // added to the rows that do.
                 if (edge(t)) {
@@ -328,13 +384,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_chunk_kernel(PagedAttent
                     }
                 }
             }
-            store_k(t + 1, pages_next, kw);
-            store_v(t + 1, vw);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) pages_next[e] = pages_far[e];
-            load(a.c.K, t + 2, pages_next, kw);
-            load(a.c.V, t + 2, pages_next, vw);
+            store(t + 1, next, kw, vw);
+            next[0] = far[0];
+            next[1] = far[1];
+            load(t + 2, next, kw, vw);
             workgroup_sync();
+            }
         }
 
         const float l = over_halves_sum(st.l);

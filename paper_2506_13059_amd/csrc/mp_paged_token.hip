@@ -59,16 +59,20 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
     const int vr = 4 * g + (col >> 2);
     const uint32_t v_at = ring + kPiece + (uint32_t)(vr * 256 + ((((col & 3) >> 1) ^ ((vr & 7) << 1)) << 4) + (col & 1) * 8);      // ^ 32 d
 
-    auto page_at = [&](int t) {              // of key 32 t + lane % 32
-        const int key = t * kTile + (lane & 31);
-        return t < t1 && key < c.end ? page_of(c.entries, c.stride, c.n_pages, c.shift, key) : -1;
-    };
+    // (entries are looked at two tiles after they were asked for: looked at at once, they made the wave wait for all loads before them)
+    auto entry_at = [&](int t) { return c.entries[min(t * kTile + (lane & 31), c.end - 1) >> c.shift]; };      // of key 32 t + lane % 32
+    auto held = [&](int t, int entry) { return (uint32_t)__ballot(t * kTile + (lane & 31) < c.end && (uint32_t)entry < (uint32_t)c.n_pages); };
     long long off[8];
-    auto offsets = [&](int t, int page) {    // bytes, of rows 4 i + g
+    auto offsets = [&](int t, int entry, uint32_t valid) {    // bytes, of rows 4 i + g; those that are not there: somewhere in page 0
+        if (c.shift >= 5) {                  // (the tile lies in one page)
+            const int page = valid ? __builtin_amdgcn_readfirstlane(entry) : 0;
+            const long long at = row_of(page, c.h, c.n_kv, c.shift, t * kTile) * 256 + g * 256;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int p = max(__shfl(page, 4 * i + g, 64), 0);
-            off[i] = row_of(p, c.h, c.n_kv, c.shift, t * kTile + 4 * i + g) * 256;
+            for (int i = 0; i < 8; ++i) off[i] = at + i * 1024;
+        } else {
+            const int mine = (valid >> (lane & 31) & 1) ? entry : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) off[i] = row_of(__shfl(mine, 4 * i + g, 64), c.h, c.n_kv, c.shift, t * kTile + 4 * i + g) * 256;
         }
     };
     auto load_keys = [&](int t) {
@@ -82,16 +86,16 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
 
     // Loads come back in order: K V K V ..., eight instructions a piece, and one for the pages of a tile four ahead now and then; "at most as many on their
     // way as the pieces behind it have" means that a piece is there.  Nothing is asked for past the end.
-    int pages[4];
+    int entries[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) pages[i] = page_at(t0 + i);
-    uint32_t valid0 = (uint32_t)__ballot(pages[0] >= 0), valid1 = 0;
-    offsets(t0, pages[0]);
+    for (int i = 0; i < 4; ++i) entries[i] = entry_at(t0 + i);
+    uint32_t valid0 = held(t0, entries[0]), valid1 = 0;
+    offsets(t0, entries[0], valid0);
     load_keys(t0);
     load_values(t0);
     if (t0 + 1 < t1) {
-        valid1 = (uint32_t)__ballot(pages[1] >= 0);
-        offsets(t0 + 1, pages[1]);
+        valid1 = held(t0 + 1, entries[1]);
+        offsets(t0 + 1, entries[1], valid1);
         load_keys(t0 + 1);
         load_values(t0 + 1);
     }
@@ -110,11 +114,11 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
                      : "v"(a0), "v"(a1), "v"(a2), "v"(a3)
                      : "memory");
         if constexpr (kAhead == 2) {
-            valid1 = (uint32_t)__ballot(pages[2] >= 0);
-            offsets(t + 2, pages[2]);
+            valid1 = held(t + 2, entries[2]);
+            offsets(t + 2, entries[2], valid1);
             load_keys(t + 2);
-            pages[2] = pages[3];
-            pages[3] = page_at(t + 4);
+            entries[2] = entries[3];
+            entries[3] = entry_at(t + 4);
         }
         f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
