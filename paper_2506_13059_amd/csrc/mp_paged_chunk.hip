@@ -1,7 +1,7 @@
 // Attention of many new tokens over a paged cache, on the matrix cores, for gfx950.  (mp_paged_attn.hip says what is computed.)
 //
-// Eight waves of 32 query rows each work on one item (mp_paged_plan.h): 64 keys and values at a time are brought to LDS by all of them, through registers, a block
-// ahead.  S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16, so a lane holds one query row in both (its column): its softmax
+// Eight waves of 32 query rows each work on one item (mp_paged_plan.h): 64 keys and values at a time go straight to LDS (global_load_lds, 16 bytes a lane), into
+// a ring of four blocks, up to three blocks ahead.  S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16, so a lane holds one query row in both (its column): its softmax
 // needs no more of other lanes than one exchange of maxima, and the rows of S^T that it holds are, converted to bf16, what the second product takes from it,
 // with the values' rows read (transposed by LDS) in the same order.
 #include "mp_paged_plan.h"
@@ -20,15 +20,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
 constexpr int kWaves = 8, kKeys = 64, kRows = 32 * kWaves;
-constexpr int kBlockBytes = kKeys * 256;
+constexpr int kRing = 4, kPiece = kKeys * 256, kBlockBytes = 2 * kPiece;      // LDS: blocks, keys and then values of one
 constexpr int kWorkgroups = 256;
 constexpr int kPartFloats = kRows * kHeadDim + 2 * kRows;       // a part: weighted values as the lanes hold them, then maxima, then sums
 
-template <typename T>
-__device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t at)
-{
-    return reinterpret_cast<__attribute__((address_space(3))) T*>((uintptr_t)at);
-}
 __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(lds_byte*)p; }
 
 struct Softmax {
@@ -47,12 +42,65 @@ __device__ __forceinline__ float over_halves_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// (what a wave has asked of LDS it has waited for by then)
 __device__ __forceinline__ void workgroup_sync()
 {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    asm volatile("" ::: "memory");
 }
+
+__device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds_off)
+{
+    // (the LDS address is the same in all lanes; lane i's bytes go to it + 16 i)
+    auto* dst = reinterpret_cast<__attribute__((address_space(3))) uint32_t*>((uintptr_t)lds_off);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src, dst, 16, 0, 0);
+}
+template <int N>
+__device__ __forceinline__ void wait_vm()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// LDS is read and written by hand: the compiler would have each access wait for every load to LDS that is on its way.
+// Keys: chunks at a[0] .. a[3] of rows r and 32 + r.
+__device__ __forceinline__ void read_keys(bf16x8 (&k)[8], const uint32_t (&a)[4])
+{
+    asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:8192\n\tds_read_b128 %2, %9\n\tds_read_b128 %3, %9 offset:8192\n\t"
+                 "ds_read_b128 %4, %10\n\tds_read_b128 %5, %10 offset:8192\n\tds_read_b128 %6, %11\n\tds_read_b128 %7, %11 offset:8192\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(k[4]), "=&v"(k[5]), "=&v"(k[6]), "=&v"(k[7])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3])
+                 : "memory");
+}
+// Values of 32 keys, transposed: v[4 s + d] has dims 32 d .. of 16 keys from 16 s.
+__device__ __forceinline__ void read_values(s16x4 (&v)[16], const uint32_t (&a)[4])
+{
+    asm volatile("ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:2048\n\tds_read_b64_tr_b16 %2, %17\n\t"
+                 "ds_read_b64_tr_b16 %3, %17 offset:2048\n\tds_read_b64_tr_b16 %4, %18\n\tds_read_b64_tr_b16 %5, %18 offset:2048\n\t"
+                 "ds_read_b64_tr_b16 %6, %19\n\tds_read_b64_tr_b16 %7, %19 offset:2048\n\t"
+                 "ds_read_b64_tr_b16 %8, %16 offset:4096\n\tds_read_b64_tr_b16 %9, %16 offset:6144\n\tds_read_b64_tr_b16 %10, %17 offset:4096\n\t"
+                 "ds_read_b64_tr_b16 %11, %17 offset:6144\n\tds_read_b64_tr_b16 %12, %18 offset:4096\n\tds_read_b64_tr_b16 %13, %18 offset:6144\n\t"
+                 "ds_read_b64_tr_b16 %14, %19 offset:4096\n\tds_read_b64_tr_b16 %15, %19 offset:6144\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]), "=&v"(v[8]), "=&v"(v[9]),
+                   "=&v"(v[10]), "=&v"(v[11]), "=&v"(v[12]), "=&v"(v[13]), "=&v"(v[14]), "=&v"(v[15])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3])
+                 : "memory");
+}
+__device__ __forceinline__ u32x4 lds_read16(uint32_t at)
+{
+    u32x4 w;
+    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(at) : "memory");
+    return w;
+}
+__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 w) { asm volatile("ds_write_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" ::"v"(at), "v"(w) : "memory"); }
+__device__ __forceinline__ unsigned long long lds_read8(uint32_t at)        // the same in all lanes
+{
+    unsigned long long w;
+    asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(at) : "memory");
+    return (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(w >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)w);
+}
+__device__ __forceinline__ void lds_write1(uint32_t at, uint32_t v) { asm volatile("ds_write_b8 %0, %1\n\ts_waitcnt lgkmcnt(0)" ::"v"(at), "v"(v) : "memory"); }
 
 // The lowest n of 64 bits.
 __device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
@@ -91,12 +139,12 @@ __device__ __forceinline__ void store_part(float* part, const Softmax& st, float
     }
 }
 
+// kOnePage: pages of eight rows or more.
+template <bool kOnePage>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
 {
-    __shared__ __align__(256) unsigned char lds_k[2][kBlockBytes];
-    __shared__ __align__(256) unsigned char lds_v[2][kBlockBytes];
-    __shared__ __align__(8) unsigned char lds_valid[2][kWaves];      // keys that are there, a bit each
-    __shared__ __align__(8) unsigned char lds_odd[2][kWaves];        // ... of an edge's block, whose values are not all finite
+    __shared__ __align__(256) unsigned char lds[kRing * kBlockBytes + 2 * kRing * kWaves];
+    const uint32_t ring = lds_offset(lds), valid_at = ring + kRing * kBlockBytes, odd_at = valid_at + kRing * kWaves;      // (a byte a wave: keys that are there; whose values are not all finite)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
     const Line line = line_of(a, tl);
     const int share = share_of(line, blockIdx.x);
@@ -107,27 +155,21 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const float scale = a.scale_log2e;
     const int G = tl.group;
 
-    // LDS addresses: of the lane's row in the first 32 keys, chunk 2 ks + half; of its place in the first 16 values, dims 32 d; and of what it loads
-    uint32_t k_at[8], v_at[4], k_to, v_to;
+    // LDS addresses in the first block: of the lane's row among 32 keys, chunk 2 ks + half (of ks = 0); of its place among 16 values (of dims 32 d); where the
+    // wave's loads go; and what a lane loads, in bytes from the wave's first row.  Chunk j (16 bytes) of row k lies at j ^ k % 16 (keys) or j ^ 4 (k % 4)
+    // (values): what the lanes of a read touch together lies in different banks.
+    uint32_t k_at, v_at[4], k_from, v_from;
     {
-        const int g = lane >> 4, c = lane & 15;
-        k_to = lds_offset(lds_k) + (8 * wave + g) * 256 + ((c ^ (8 * (wave & 1) + g)) << 4);
-        v_to = lds_offset(lds_v) + (8 * wave + g) * 256 + ((c ^ (g << 2)) << 4);
-        const int row = lane & 31, v_row = 4 * half + ((lane & 15) >> 2);
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) k_at[ks] = lds_offset(lds_k) + row * 256 + (((2 * ks + half) ^ (row & 15)) << 4);
+        const int g = lane >> 4, c = lane & 15, v_row = 4 * half + (c >> 2);
+        k_at = ring + (lane & 31) * 256 + ((half ^ c) << 4);
 #pragma unroll
         for (int d = 0; d < 4; ++d)
-            v_at[d] = lds_offset(lds_v) + v_row * 256 + (((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ ((v_row & 3) << 2)) << 4) + (lane & 1) * 8;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(k_at[ks]));
-#pragma unroll
-        for (int d = 0; d < 4; ++d) asm volatile("" : "+v"(v_at[d]));
+            v_at[d] = ring + kPiece + v_row * 256 + (((4 * d + 2 * (g & 1) + ((c & 3) >> 1)) ^ ((v_row & 3) << 2)) << 4) + (c & 1) * 8;
+        k_from = g * 256 + ((c ^ (8 * (wave & 1) + g)) << 4);
+        v_from = g * 256 + ((c ^ (g << 2)) << 4);
     }
+    const uint32_t wave_at = ring + 8 * wave * 256;
 
-#ifdef PRIO
-    if (wave < 4) __builtin_amdgcn_s_setprio(PRIO);
-#endif
     long long x = share * line.share;
     const long long x_end = min(x + line.share, line.all);
     Cut cut{};
@@ -153,46 +195,47 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(bf16x8, from[2 * ks + half]);
         }
 
-        // Loading: rows 8 wave + 4 e + lane / 16 of a block, chunk lane % 16 of 16 bytes.  In LDS chunk j of row k lies at j ^ k % 16 (keys) or j ^ 4 (k % 4)
-        // (values): what the lanes of a read touch together lies in different banks.  Pages of eight rows or more hold all that a wave loads of a
-        // block, so its address is a scalar.
+        // Loading: a wave brings rows 8 wave .. + 7 of a block, two times two instructions of four rows.  Pages of eight rows or more hold all of them, so their
+        // address is a scalar.
         const int32_t* entries = a.c.table + (long long)it.b * a.c.table_stride;
-        const int chunk = lane & 15;
+        typedef const __attribute__((address_space(4))) int32_t constant_int;
         const int end = min(it.rows.base + it.rows.n, room_of(a));       // keys of the sequence
-        const bool one_page = a.c.page_shift >= 3;
-        // (entries are looked at a block after they were asked for: looked at at once, they made a wave wait for all loads before them)
-        auto entry_at = [&](int block, int (&entry)[2]) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (e == 1 && one_page) break;
-                const int key = block * kKeys + 8 * wave + (one_page ? 0 : 4 * e + (lane >> 4));
-                entry[e] = entries[min(key, end - 1) >> a.c.page_shift];
-            }
-        };
-        auto held = [&](int entry, int key) { return key < end && (uint32_t)entry < (uint32_t)a.c.n_pages; };
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        // One block's rows of this wave; what is not there keeps what the registers held.
-        auto load = [&](int block, const int (&entry)[2], uint4 (&kw)[2], uint4 (&vw)[2]) {
+        // What a wave needs to know of the rows that it loads: the entry (or, for small pages, one of each row in lanes 8 r ..).
+        auto entry_at = [&](int block) {
             const int key = block * kKeys + 8 * wave;
-            if (one_page) {
-                const int page = __builtin_amdgcn_readfirstlane(entry[0]);
-                if (held(page, key)) {
-                    const long long at = row_of(page, h, a.c.n_kv, a.c.page_shift, key) * 16;
-                    const uint4 *k = reinterpret_cast<const uint4*>(a.c.K) + at, *v = reinterpret_cast<const uint4*>(a.c.V) + at;
-                    kw[0] = k[(uint32_t)lane];
-                    kw[1] = k[(uint32_t)lane + 64];
-                    vw[0] = v[(uint32_t)lane];
-                    vw[1] = v[(uint32_t)lane + 64];
-                }
+            if constexpr (kOnePage) return (int)((constant_int*)entries)[min(key, end - 1) >> a.c.page_shift];
+            else return (int)entries[min(key + (lane >> 3), end - 1) >> a.c.page_shift];
+        };
+        // A bit for each of them that is there.
+        auto bits_of = [&](int block, int entry) {
+            const int n = end - (block * kKeys + 8 * wave);
+            const uint32_t in = n >= 8 ? 255u : n > 0 ? (1u << n) - 1u : 0u;
+            if constexpr (kOnePage) return (uint32_t)__builtin_amdgcn_readfirstlane(entry) < (uint32_t)a.c.n_pages ? in : 0u;
+            const unsigned long long ok = __ballot((uint32_t)entry < (uint32_t)a.c.n_pages);
+            uint32_t held = 0;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) held |= (uint32_t)(ok >> (8 * r) & 1) << r;
+            return in & held;
+        };
+        // Four instructions; rows that are not there: those of page 0.
+        auto load = [&](int block, int entry, uint32_t bits) {
+            const int key = block * kKeys + 8 * wave;
+            const uint32_t to = wave_at + (uint32_t)((block & (kRing - 1)) * kBlockBytes);
+            if constexpr (kOnePage) {
+                const int page = bits ? __builtin_amdgcn_readfirstlane(entry) : 0;
+                const long long at = row_of(page, h, a.c.n_kv, a.c.page_shift, key) * 256;
+                const unsigned char *k = reinterpret_cast<const unsigned char*>(a.c.K) + at, *v = reinterpret_cast<const unsigned char*>(a.c.V) + at;
+                load_to_lds(k + k_from, to);
+                load_to_lds(k + ((k_from ^ 64u) + 1024u), to + 1024);
+                load_to_lds(v + v_from, to + kPiece);
+                load_to_lds(v + (v_from + 1024u), to + kPiece + 1024);
             } else {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int row_key = key + 4 * e + (lane >> 4);
-                    if (held(entry[e], row_key)) {
-                        const long long at = row_of(entry[e], h, a.c.n_kv, a.c.page_shift, row_key) * 16 + chunk;
-                        kw[e] = reinterpret_cast<const uint4*>(a.c.K)[at];
-                        vw[e] = reinterpret_cast<const uint4*>(a.c.V)[at];
-                    }
+                    const int r = 4 * e + (lane >> 4), page = __shfl(entry, 8 * r, 64);
+                    const long long at = row_of((bits >> r & 1) ? page : 0, h, a.c.n_kv, a.c.page_shift, key + r) * 256;
+                    load_to_lds(reinterpret_cast<const unsigned char*>(a.c.K) + at + (((e ? k_from ^ 64u : k_from)) & 255u), to + e * 1024);
+                    load_to_lds(reinterpret_cast<const unsigned char*>(a.c.V) + at + (v_from & 255u), to + kPiece + e * 1024);
                 }
             }
         };
@@ -201,80 +244,36 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             return block * kKeys + kKeys - 1 > it.rows.base + it.tile * tl.tokens ||
                    (a.window && block * kKeys <= it.rows.base + min(it.rows.n, (it.tile + 1) * tl.tokens) - 1 - a.window);
         };
-        auto store = [&](int block, const int (&entry)[2], uint4 (&kw)[2], uint4 (&vw)[2]) {
-            uint32_t bits = 0, odd = 0;
-            if (one_page) {
-                const int n = end - (block * kKeys + 8 * wave);
-                if ((uint32_t)__builtin_amdgcn_readfirstlane(entry[0]) < (uint32_t)a.c.n_pages) bits = n >= 8 ? 255u : n > 0 ? (1u << n) - 1u : 0u;
-            } else {
+        // When the wave's rows of a block have come: values of rows that are not there are zeroed (a probability of zero meets them), and so are those of an
+        // edge's block that are not finite, lest they meet the zero of a row that does not see them.
+        auto arrived = [&](int block, uint32_t bits) {
+            uint32_t odd = 0;
+            const bool at_edge = edge(block);
+            if (bits != 255u || at_edge) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const unsigned long long in = __ballot(held(entry[e], block * kKeys + 8 * wave + 4 * e + (lane >> 4)));
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) bits |= (uint32_t)(in >> (16 * k) & 1) << (4 * e + k);
-                }
-            }
-            if (bits != 255u) {              // (rows without a key are zero: a probability of zero meets them)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (!(bits >> (4 * e + (lane >> 4)) & 1)) vw[e] = zero;
-            }
-            if (edge(block)) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    uint32_t u[4] = {vw[e].x, vw[e].y, vw[e].z, vw[e].w};
+                    const uint32_t at = wave_at + (uint32_t)((block & (kRing - 1)) * kBlockBytes) + kPiece + e * 1024 + lane * 16;
+                    u32x4 w = lds_read16(at);
                     bool off_range = false;
+                    if (!(bits >> (4 * e + (lane >> 4)) & 1)) {
+                        w = u32x4{0u, 0u, 0u, 0u};
+                    } else if (at_edge) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const bool lo = (u[k] & 0x7f80u) == 0x7f80u, hi = (u[k] & 0x7f800000u) == 0x7f800000u;
-                        off_range |= lo | hi;
-                        u[k] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                        for (int k = 0; k < 4; ++k) {
+                            const bool lo = (w[k] & 0x7f80u) == 0x7f80u, hi = (w[k] & 0x7f800000u) == 0x7f800000u;
+                            off_range |= lo | hi;
+                            w[k] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                        }
                     }
-                    vw[e] = make_uint4(u[0], u[1], u[2], u[3]);
+                    lds_write16(at, w);
                     const unsigned long long in = __ballot(off_range);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) odd |= (uint32_t)((in >> (16 * k) & 0xffff) != 0) << (4 * e + k);
                 }
             }
-            if (lane == 0) {
-                lds_valid[block & 1][wave] = (unsigned char)bits;
-                lds_odd[block & 1][wave] = (unsigned char)odd;
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                *lds_at<u32x4>((e ? k_to ^ 64u : k_to) + (block & 1) * kBlockBytes + e * 1024) = u32x4{kw[e].x, kw[e].y, kw[e].z, kw[e].w};
-                *lds_at<u32x4>(v_to + (block & 1) * kBlockBytes + e * 1024) = u32x4{vw[e].x, vw[e].y, vw[e].z, vw[e].w};
-            }
-        };
-
-        // (reads kAhead ahead of the products that take them: left alone, the compiler has each product wait for a read of its own)
-        auto scores = [&](int block, f32x16 (&s)[2]) {
-#ifndef KA
-#define KA 4
-#endif
-            constexpr int kAhead = KA;
-            bf16x8 k[kAhead];
-            auto read = [&](int i) { k[i % kAhead] = *lds_at<bf16x8>(k_at[i >> 1] + (block & 1) * kBlockBytes + (i & 1) * 32 * 256); };
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) read(i);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i % kAhead], q[i >> 1], s[i & 1], 0, 0, 0);
-                if (i + kAhead < 16) read(i + kAhead);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        };
-        // 16 keys from 16 s and 32 dims from 32 d of the values, transposed: keys 4 half .. + 3, then 8 + 4 half .. + 3, of the lane's dim
-        auto values = [&](int block, int s, int d) {
-            auto* p = lds_at<s16x4>(v_at[d] + (block & 1) * kBlockBytes + s * 16 * 256);
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(v_at[d] + (block & 1) * kBlockBytes + s * 16 * 256 + 8 * 256));
-            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            const uint32_t byte = (uint32_t)((block & (kRing - 1)) * kWaves + wave);
+            lds_write1(valid_at + byte, bits);
+            if (at_edge) lds_write1(odd_at + byte, odd);
         };
 
         Softmax st;
@@ -285,25 +284,48 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
             for (int j = 0; j < 16; ++j) st.o[d][j] = 0.f;
 
-        uint4 kw[2] = {zero, zero}, vw[2] = {zero, zero};
         if (end > 0) {
-            int now[2], next[2];
-            entry_at(first, now);
-            entry_at(first + 1, next);
-            load(first, now, kw, vw);
+            // what the wave knows of the rows on their way, a block ahead and more
+            uint32_t bits1, bits2 = 0, bits3 = 0;
+            int entry = entry_at(first);
+            const int entry1 = entry_at(first + 1), entry2 = entry_at(first + 2);
             workgroup_sync();                              // (the item before is done with LDS)
-            store(first, now, kw, vw);
-            load(first + 1, next, kw, vw);
+            bits1 = bits_of(first, entry);
+            load(first, entry, bits1);
+            if (first + 1 < last) load(first + 1, entry1, bits2 = bits_of(first + 1, entry1));
+            if (first + 2 < last) load(first + 2, entry2, bits3 = bits_of(first + 2, entry2));
+            entry = entry_at(first + 3);
+            if (first + 2 < last) wait_vm<8>();
+            else wait_vm<0>();
+            arrived(first, bits1);
             workgroup_sync();
             for (int t = first; t < last; ++t) {
-            int far[2];
-            entry_at(t + 2, far);
-            if (active && t * kKeys <= pos_max) {
+                const uint32_t slot = (uint32_t)((t & (kRing - 1)) * kBlockBytes);
+                // block t + 3 takes the place of block t - 1
+                bits1 = bits2;
+                bits2 = bits3;
+                if (t + 3 < last) {
+                    bits3 = bits_of(t + 3, entry);
+                    load(t + 3, entry, bits3);
+                    entry = entry_at(t + 4);
+                }
+                if (active && t * kKeys <= pos_max) {
                 f32x16 s[2];
-                scores(t, s);
-                const unsigned long long valid = *reinterpret_cast<const unsigned long long*>(lds_valid[t & 1]);
-                const uint32_t valid_lo = __builtin_amdgcn_readfirstlane((uint32_t)valid), valid_hi = __builtin_amdgcn_readfirstlane((uint32_t)(valid >> 32));
-                const bool masked = (valid_lo & valid_hi) != 0xffffffffu || t * kKeys + kKeys - 1 > pos_min || (a.window && t * kKeys <= pos_max - a.window);
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) s[tt][j] = 0.f;
+#pragma unroll
+                for (int x4 = 0; x4 < 2; ++x4) {
+                    const uint32_t b = k_at ^ (128u * x4);
+                    const uint32_t at[4] = {b + slot, (b ^ 32u) + slot, (b ^ 64u) + slot, (b ^ 96u) + slot};
+                    bf16x8 k[8];
+                    read_keys(k, at);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i], q[4 * x4 + (i >> 1)], s[i & 1], 0, 0, 0);
+                }
+                const unsigned long long valid = lds_read8(valid_at + (t & (kRing - 1)) * kWaves);
+                const bool masked = valid != ~0ull || t * kKeys + kKeys - 1 > pos_min || (a.window && t * kKeys <= pos_max - a.window);
                 if (masked) {
                     // keys (from, upto] of the block, those that are there; bit k of `see` for key 4 half + k
                     const int upto = position - t * kKeys, from = a.window ? upto - a.window : -1;
@@ -332,7 +354,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         for (int j = 0; j < 16; ++j) st.o[d][j] *= f;
                 }
                 const float m = st.m == -INFINITY ? 0.f : st.m;
-                // Probabilities of 16 keys at a time, two elements behind each product of the 16 keys before; values are read two products ahead.
+                // Probabilities of 16 keys at a time, two elements behind each product of the 16 keys before.
                 bf16x8 p[4];
                 auto probabilities = [&](int k, int e) {
 #pragma unroll
@@ -342,31 +364,26 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         p[k][j] = (__bf16)x;
                     }
                 };
-#ifndef VA
-#define VA 2
-#endif
-                constexpr int kAhead = VA;
-                s16x8 v[kAhead];
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) v[i] = values(t, 0, i);
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) probabilities(0, e);
-                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[i % kAhead]), p[i >> 2], st.o[i & 3], 0, 0, 0);
-                    if (i + kAhead < 16) v[i % kAhead] = values(t, (i + kAhead) >> 2, (i + kAhead) & 3);
-                    if (i < 12) probabilities((i >> 2) + 1, 2 * (i & 3));
-#ifndef NOSB
-                    __builtin_amdgcn_sched_barrier(0);
-#endif
+                for (int k2 = 0; k2 < 2; ++k2) {
+                    const uint32_t b = slot + 8192u * k2;
+                    const uint32_t at[4] = {v_at[0] + b, v_at[1] + b, v_at[2] + b, v_at[3] + b};
+                    s16x4 v[16];
+                    read_values(v, at);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const auto w = __builtin_shufflevector(v[2 * i], v[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                        st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p[2 * k2 + (i >> 2)], st.o[i & 3], 0, 0, 0);
+                        if (8 * k2 + i < 12) probabilities(2 * k2 + (i >> 2) + 1, 2 * (i & 3));
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
                 // Values that are not finite have been taken out of an edge's block, lest they meet the zero of a row that does not see them: they are
                 // added to the rows that do.
                 if (edge(t)) {
-                    const unsigned long long flags = *reinterpret_cast<const unsigned long long*>(lds_odd[t & 1]);
-                    unsigned long long odd = (unsigned long long)__builtin_amdgcn_readfirstlane((uint32_t)(flags >> 32)) << 32 | __builtin_amdgcn_readfirstlane((uint32_t)flags);
-                    for (; odd; odd &= odd - 1) {
+                    for (unsigned long long odd = lds_read8(odd_at + (t & (kRing - 1)) * kWaves); odd; odd &= odd - 1) {
                         const int key = t * kKeys + __ffsll((long long)odd) - 1;
                         const int page = __builtin_amdgcn_readfirstlane(page_of(entries, a.c.table_stride, a.c.n_pages, a.c.page_shift, key));
                         const bool sees = key <= position && !(a.window && key <= position - a.window);
@@ -384,11 +401,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     }
                 }
             }
-            store(t + 1, next, kw, vw);
-            next[0] = far[0];
-            next[1] = far[1];
-            load(t + 2, next, kw, vw);
-            workgroup_sync();
+                if (t + 1 < last) {
+                    if (t + 3 < last) wait_vm<8>();
+                    else if (t + 2 < last) wait_vm<4>();
+                    else wait_vm<0>();
+                    arrived(t + 1, bits1);
+                }
+                workgroup_sync();
             }
         }
 
@@ -462,7 +481,8 @@ hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, h
     const Tiling tl = chunk_tiling(a.n_q_heads / a.c.n_kv, over);
     Cut* cuts = reinterpret_cast<Cut*>(room);
     float* parts = room + kCutFloats;
-    hipLaunchKernelGGL(paged_chunk_kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
+    const auto kernel = a.c.page_shift >= 3 ? paged_chunk_kernel<true> : paged_chunk_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(8 * kWorkgroups), dim3(64), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
