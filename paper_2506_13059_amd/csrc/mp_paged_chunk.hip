@@ -56,26 +56,29 @@ __device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds_off)
     auto* dst = reinterpret_cast<__attribute__((address_space(3))) uint32_t*>((uintptr_t)lds_off);
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src, dst, 16, 0, 0);
 }
+// At most N loads on their way, and nothing asked of LDS.
 template <int N>
 __device__ __forceinline__ void wait_vm()
 {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
 // LDS is read and written by hand: the compiler would have each access wait for every load to LDS that is on its way.
-// Keys: chunks at a[0] .. a[3] of rows r and 32 + r.
-__device__ __forceinline__ void read_keys(bf16x8 (&k)[8], const uint32_t (&a)[4])
+// Keys: the 16 bytes at a ^ 32 ks (ks = 0 .. 3), and 32 rows on: k[2 ks], k[2 ks + 1].
+__device__ __forceinline__ void read_keys(bf16x8 (&k)[8], uint32_t a, uint32_t slot)
 {
+    const uint32_t a0 = a + slot, a1 = (a ^ 32u) + slot, a2 = (a ^ 64u) + slot, a3 = (a ^ 96u) + slot;
     asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:8192\n\tds_read_b128 %2, %9\n\tds_read_b128 %3, %9 offset:8192\n\t"
                  "ds_read_b128 %4, %10\n\tds_read_b128 %5, %10 offset:8192\n\tds_read_b128 %6, %11\n\tds_read_b128 %7, %11 offset:8192\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(k[4]), "=&v"(k[5]), "=&v"(k[6]), "=&v"(k[7])
-                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3])
+                 : "v"(a0), "v"(a1), "v"(a2), "v"(a3)
                  : "memory");
 }
-// Values of 32 keys, transposed: v[4 s + d] has dims 32 d .. of 16 keys from 16 s.
-__device__ __forceinline__ void read_values(s16x4 (&v)[16], const uint32_t (&a)[4])
+// Values of 32 keys, transposed: v[2 (4 s + d)], v[2 (4 s + d) + 1] have dims 32 d .. of 16 keys from 16 s.
+__device__ __forceinline__ void read_values(s16x4 (&v)[16], uint32_t a, uint32_t slot)
 {
+    const uint32_t a0 = a + slot, a1 = (a ^ 64u) + slot, a2 = (a ^ 128u) + slot, a3 = (a ^ 192u) + slot;
     asm volatile("ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:2048\n\tds_read_b64_tr_b16 %2, %17\n\t"
                  "ds_read_b64_tr_b16 %3, %17 offset:2048\n\tds_read_b64_tr_b16 %4, %18\n\tds_read_b64_tr_b16 %5, %18 offset:2048\n\t"
                  "ds_read_b64_tr_b16 %6, %19\n\tds_read_b64_tr_b16 %7, %19 offset:2048\n\t"
@@ -84,7 +87,7 @@ __device__ __forceinline__ void read_values(s16x4 (&v)[16], const uint32_t (&a)[
                  "ds_read_b64_tr_b16 %14, %19 offset:4096\n\tds_read_b64_tr_b16 %15, %19 offset:6144\n\ts_waitcnt lgkmcnt(0)"
                  : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]), "=&v"(v[8]), "=&v"(v[9]),
                    "=&v"(v[10]), "=&v"(v[11]), "=&v"(v[12]), "=&v"(v[13]), "=&v"(v[14]), "=&v"(v[15])
-                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3])
+                 : "v"(a0), "v"(a1), "v"(a2), "v"(a3)
                  : "memory");
 }
 __device__ __forceinline__ u32x4 lds_read16(uint32_t at)
@@ -100,7 +103,8 @@ __device__ __forceinline__ unsigned long long lds_read8(uint32_t at)        // t
     asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(at) : "memory");
     return (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(w >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)w);
 }
-__device__ __forceinline__ void lds_write1(uint32_t at, uint32_t v) { asm volatile("ds_write_b8 %0, %1\n\ts_waitcnt lgkmcnt(0)" ::"v"(at), "v"(v) : "memory"); }
+// (not waited for: the wave's next read is)
+__device__ __forceinline__ void lds_write1(uint32_t at, uint32_t v) { asm volatile("ds_write_b8 %0, %1" ::"v"(at), "v"(v) : "memory"); }
 
 // The lowest n of 64 bits.
 __device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
@@ -155,16 +159,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const float scale = a.scale_log2e;
     const int G = tl.group;
 
-    // LDS addresses in the first block: of the lane's row among 32 keys, chunk 2 ks + half (of ks = 0); of its place among 16 values (of dims 32 d); where the
+    // LDS addresses in the first block: of the lane's row among 32 keys, chunk 2 ks + half (of ks = 0); of its place among 16 values (of dims 32 d, d = 0); where the
     // wave's loads go; and what a lane loads, in bytes from the wave's first row.  Chunk j (16 bytes) of row k lies at j ^ k % 16 (keys) or j ^ 4 (k % 4)
     // (values): what the lanes of a read touch together lies in different banks.
-    uint32_t k_at, v_at[4], k_from, v_from;
+    uint32_t k_at, v_at, k_from, v_from;
     {
         const int g = lane >> 4, c = lane & 15, v_row = 4 * half + (c >> 2);
         k_at = ring + (lane & 31) * 256 + ((half ^ c) << 4);
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-            v_at[d] = ring + kPiece + v_row * 256 + (((4 * d + 2 * (g & 1) + ((c & 3) >> 1)) ^ ((v_row & 3) << 2)) << 4) + (c & 1) * 8;
+        v_at = ring + kPiece + v_row * 256 + (((2 * (g & 1) + ((c & 3) >> 1)) ^ ((v_row & 3) << 2)) << 4) + (c & 1) * 8;
         k_from = g * 256 + ((c ^ (8 * (wave & 1) + g)) << 4);
         v_from = g * 256 + ((c ^ (g << 2)) << 4);
     }
@@ -217,33 +219,46 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             for (int r = 0; r < 8; ++r) held |= (uint32_t)(ok >> (8 * r) & 1) << r;
             return in & held;
         };
-        // Four instructions; rows that are not there: those of page 0.
-        auto load = [&](int block, int entry, uint32_t bits) {
+        // Four instructions, two of keys and two of values; rows that are not there: those of page 0.
+        struct Rows {
+            const unsigned char *k[2], *v[2];      // from here, a lane each
+            uint32_t to;
+        };
+        auto rows_at = [&](int block, int place, int entry, uint32_t bits) {
             const int key = block * kKeys + 8 * wave;
-            const uint32_t to = wave_at + (uint32_t)((block & (kRing - 1)) * kBlockBytes);
+            Rows r;
+            r.to = wave_at + (uint32_t)((place & (kRing - 1)) * kBlockBytes);
+            lds_write1(valid_at + (uint32_t)((place & (kRing - 1)) * kWaves + wave), bits);
             if constexpr (kOnePage) {
                 const int page = bits ? __builtin_amdgcn_readfirstlane(entry) : 0;
                 const long long at = row_of(page, h, a.c.n_kv, a.c.page_shift, key) * 256;
-                const unsigned char *k = reinterpret_cast<const unsigned char*>(a.c.K) + at, *v = reinterpret_cast<const unsigned char*>(a.c.V) + at;
-                load_to_lds(k + k_from, to);
-                load_to_lds(k + ((k_from ^ 64u) + 1024u), to + 1024);
-                load_to_lds(v + v_from, to + kPiece);
-                load_to_lds(v + (v_from + 1024u), to + kPiece + 1024);
+                r.k[0] = r.k[1] = reinterpret_cast<const unsigned char*>(a.c.K) + at;
+                r.v[0] = r.v[1] = reinterpret_cast<const unsigned char*>(a.c.V) + at;
             } else {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = 4 * e + (lane >> 4), page = __shfl(entry, 8 * r, 64);
-                    const long long at = row_of((bits >> r & 1) ? page : 0, h, a.c.n_kv, a.c.page_shift, key + r) * 256;
-                    load_to_lds(reinterpret_cast<const unsigned char*>(a.c.K) + at + (((e ? k_from ^ 64u : k_from)) & 255u), to + e * 1024);
-                    load_to_lds(reinterpret_cast<const unsigned char*>(a.c.V) + at + (v_from & 255u), to + kPiece + e * 1024);
+                    const int n = 4 * e + (lane >> 4), page = __shfl(entry, 8 * n, 64);
+                    const long long at = row_of((bits >> n & 1) ? page : 0, h, a.c.n_kv, a.c.page_shift, key + n) * 256 - n * 256;
+                    r.k[e] = reinterpret_cast<const unsigned char*>(a.c.K) + at;
+                    r.v[e] = reinterpret_cast<const unsigned char*>(a.c.V) + at;
                 }
             }
+            return r;
         };
-        // a block in which some row of the item sees a key that another one does not
-        auto edge = [&](int block) {
-            return block * kKeys + kKeys - 1 > it.rows.base + it.tile * tl.tokens ||
-                   (a.window && block * kKeys <= it.rows.base + min(it.rows.n, (it.tile + 1) * tl.tokens) - 1 - a.window);
+        auto load = [&](const Rows& r, int i) {
+            if (i == 0) load_to_lds(r.k[0] + k_from, r.to);
+            if (i == 1) load_to_lds(r.k[1] + ((k_from ^ 64u) + 1024u), r.to + 1024);
+            if (i == 2) load_to_lds(r.v[0] + v_from, r.to + kPiece);
+            if (i == 3) load_to_lds(r.v[1] + (v_from + 1024u), r.to + kPiece + 1024);
         };
+        auto load_all = [&](const Rows& r) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load(r, i);
+        };
+        // Blocks in which some row of the item sees a key that another one does not: those from edge_from on, and with a window those up to edge_upto.
+        const int low = it.rows.base + it.tile * tl.tokens, high = it.rows.base + min(it.rows.n, (it.tile + 1) * tl.tokens) - 1;
+        const int edge_from = low < 0 ? -1 : (low + 1) / kKeys, edge_upto = a.window && high >= a.window ? (high - a.window) / kKeys : -1;
+        auto edge = [&](int block) { return block >= edge_from || block <= edge_upto; };
         // When the wave's rows of a block have come: values of rows that are not there are zeroed (a probability of zero meets them), and so are those of an
         // edge's block that are not finite, lest they meet the zero of a row that does not see them.
         auto arrived = [&](int block, uint32_t bits) {
@@ -271,9 +286,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     for (int k = 0; k < 4; ++k) odd |= (uint32_t)((in >> (16 * k) & 0xffff) != 0) << (4 * e + k);
                 }
             }
-            const uint32_t byte = (uint32_t)((block & (kRing - 1)) * kWaves + wave);
-            lds_write1(valid_at + byte, bits);
-            if (at_edge) lds_write1(odd_at + byte, odd);
+            if (at_edge) {
+                lds_write1(odd_at + (uint32_t)((block & (kRing - 1)) * kWaves + wave), odd);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
         };
 
         Softmax st;
@@ -288,43 +304,58 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             // what the wave knows of the rows on their way, a block ahead and more
             uint32_t bits1, bits2 = 0, bits3 = 0;
             int entry = entry_at(first);
-            const int entry1 = entry_at(first + 1), entry2 = entry_at(first + 2);
+            const int entry1 = entry_at(min(first + 1, last - 1)), entry2 = entry_at(min(first + 2, last - 1));
             workgroup_sync();                              // (the item before is done with LDS)
             bits1 = bits_of(first, entry);
-            load(first, entry, bits1);
-            if (first + 1 < last) load(first + 1, entry1, bits2 = bits_of(first + 1, entry1));
-            if (first + 2 < last) load(first + 2, entry2, bits3 = bits_of(first + 2, entry2));
-            entry = entry_at(first + 3);
-            if (first + 2 < last) wait_vm<8>();
-            else wait_vm<0>();
+            load_all(rows_at(first, first, entry, bits1));
+            int block = min(first + 1, last - 1);
+            bits2 = bits_of(block, entry1);
+            load_all(rows_at(block, first + 1, entry1, bits2));
+            block = min(first + 2, last - 1);
+            bits3 = bits_of(block, entry2);
+            load_all(rows_at(block, first + 2, entry2, bits3));
+            block = min(first + 3, last - 1);
+            entry = entry_at(block);
+            wait_vm<8>();
             arrived(first, bits1);
             workgroup_sync();
             for (int t = first; t < last; ++t) {
                 const uint32_t slot = (uint32_t)((t & (kRing - 1)) * kBlockBytes);
-                // block t + 3 takes the place of block t - 1
+                // Block t + 3 takes the place of block t - 1.  A wave's four loads are spread over its products: eight waves' loads take the memory path some
+                // 500 cycles, in which a wave that asks for more has to stand.
                 bits1 = bits2;
                 bits2 = bits3;
-                if (t + 3 < last) {
-                    bits3 = bits_of(t + 3, entry);
-                    load(t + 3, entry, bits3);
-                    entry = entry_at(t + 4);
-                }
-                if (active && t * kKeys <= pos_max) {
+                // (Past the share's end the last block is loaded again: a branch for that would cut the products' code into pieces.)
+                bits3 = bits_of(block, entry);
+                const Rows coming = rows_at(block, t + 3, entry, bits3);
+                block = min(t + 4, last - 1);
+                entry = entry_at(block);
+                // (with this as the `else` of what follows, its state was copied at the end of both, and registers ran out)
+                const bool sees_some = active && t * kKeys <= pos_max;
+                if (!sees_some) load_all(coming);
+                if (sees_some) {
+                // (keys and values are read a half at a time: with all of a block's keys at once, registers run out)
+                bf16x8 k[8];
+                read_keys(k, k_at, slot);
                 f32x16 s[2];
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) s[tt][j] = 0.f;
 #pragma unroll
-                for (int x4 = 0; x4 < 2; ++x4) {
-                    const uint32_t b = k_at ^ (128u * x4);
-                    const uint32_t at[4] = {b + slot, (b ^ 32u) + slot, (b ^ 64u) + slot, (b ^ 96u) + slot};
-                    bf16x8 k[8];
-                    read_keys(k, at);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i], q[4 * x4 + (i >> 1)], s[i & 1], 0, 0, 0);
+                for (int i = 0; i < 16; ++i) {
+                    if (i == 8) read_keys(k, k_at ^ 128u, slot);
+                    s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i & 7], q[i >> 1], s[i & 1], 0, 0, 0);
+                    if ((i & 7) == 3) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        load(coming, i >> 3);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-                const unsigned long long valid = lds_read8(valid_at + (t & (kRing - 1)) * kWaves);
+                __builtin_amdgcn_sched_barrier(0);
+                s16x4 v[16];
+                read_values(v, v_at, slot);
+                const unsigned long long valid = lds_read8(valid_at + (uint32_t)((t & (kRing - 1)) * kWaves));
                 const bool masked = valid != ~0ull || t * kKeys + kKeys - 1 > pos_min || (a.window && t * kKeys <= pos_max - a.window);
                 if (masked) {
                     // keys (from, upto] of the block, those that are there; bit k of `see` for key 4 half + k
@@ -337,11 +368,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         for (int j = 0; j < 16; ++j) s[tt][j] = in & (1u << (8 * (j >> 2) + (j & 3))) ? s[tt][j] : -INFINITY;
                     }
                 }
-                float mx = s[0][0];
+                float part[4];
 #pragma unroll
-                for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s[0][j]);
+                for (int j = 0; j < 4; ++j) part[j] = fmaxf(s[0][j], s[1][j]);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[1][j]);
+                for (int j = 4; j < 16; ++j) part[j & 3] = fmaxf(part[j & 3], fmaxf(s[0][j], s[1][j]));
+                float mx = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
                 mx = over_halves_max(mx) * scale;
                 // The maximum in use may be up to 2^8 behind: sums in fp32 and products of bf16 have room for it, and it is soon never moved.
                 if (__any(mx > st.m + 8.f)) {
@@ -367,18 +399,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) probabilities(0, e);
 #pragma unroll
-                for (int k2 = 0; k2 < 2; ++k2) {
-                    const uint32_t b = slot + 8192u * k2;
-                    const uint32_t at[4] = {v_at[0] + b, v_at[1] + b, v_at[2] + b, v_at[3] + b};
-                    s16x4 v[16];
-                    read_values(v, at);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const auto w = __builtin_shufflevector(v[2 * i], v[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-                        st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p[2 * k2 + (i >> 2)], st.o[i & 3], 0, 0, 0);
-                        if (8 * k2 + i < 12) probabilities(2 * k2 + (i >> 2) + 1, 2 * (i & 3));
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    if (i == 8) read_values(v, v_at, slot + 8192u);
+                    const auto w = __builtin_shufflevector(v[2 * (i & 7)], v[2 * (i & 7) + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p[i >> 2], st.o[i & 3], 0, 0, 0);
+                    if (i < 12) probabilities((i >> 2) + 1, 2 * (i & 3));
+                    if ((i & 7) == 3) load(coming, 2 + (i >> 3));
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 // Values that are not finite have been taken out of an edge's block, lest they meet the zero of a row that does not see them: they are
                 // added to the rows that do.
@@ -401,14 +428,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     }
                 }
             }
-                if (t + 1 < last) {
-                    if (t + 3 < last) wait_vm<8>();
-                    else if (t + 2 < last) wait_vm<4>();
-                    else wait_vm<0>();
-                    arrived(t + 1, bits1);
-                }
+                wait_vm<8>();
+                if (t + 1 < last) arrived(t + 1, bits1);
                 workgroup_sync();
             }
+            wait_vm<0>();
         }
 
         const float l = over_halves_sum(st.l);
