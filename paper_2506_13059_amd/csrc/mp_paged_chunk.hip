@@ -109,24 +109,38 @@ __device__ __forceinline__ void lds_write1(uint32_t at, uint32_t v) { asm volati
 // The lowest n of 64 bits.
 __device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY; }
+
+// A lane's dims 32 d + 8 j + 4 half .. of a finished row, o[j] over l.
+__device__ __forceinline__ void store_dims(const PagedAttention& a, long long row, int d, int half, const f32x4 (&o)[4], float l)
+{
+    const float f = l > 0.f ? 1.f / l : 0.f;
+    unsigned char* out = reinterpret_cast<unsigned char*>(a.out) + row * 256 + half * 8 + d * 64;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        bf16x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (__bf16)(l > 0.f ? o[j][e] * f : 0.f);
+        *reinterpret_cast<bf16x4*>(out + j * 16) = w;
+    }
+}
+
 // The rows of a finished item.
 __device__ __forceinline__ void store_rows(const PagedAttention& a, const Softmax& st, float l, int token, int head, bool there)
 {
     const int half = (threadIdx.x & 63) >> 5;
     if (!there) return;
-    const float f = l > 0.f ? 1.f / l : 0.f;
     const long long row = (long long)token * a.n_q_heads + head;
-    unsigned char* out = reinterpret_cast<unsigned char*>(a.out) + row * 256 + half * 8;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 4; ++d) {
+        f32x4 o[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            bf16x4 w;
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = (__bf16)(l > 0.f ? st.o[d][4 * j + e] * f : 0.f);
-            *reinterpret_cast<bf16x4*>(out + d * 64 + j * 16) = w;
-        }
-    if (a.lse && half == 0) a.lse[row] = l > 0.f ? (st.m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+            for (int e = 0; e < 4; ++e) o[j][e] = st.o[d][4 * j + e];
+        store_dims(a, row, d, half, o, l);
+    }
+    if (a.lse && half == 0) a.lse[row] = lse_of(st.m, l);
 }
 
 __device__ __forceinline__ void store_part(float* part, const Softmax& st, float l)
@@ -175,12 +189,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     long long x = share * line.share;
     const long long x_end = min(x + line.share, line.all);
     Cut cut{};
-    while (x < x_end) {
-        const int h = (int)(x / line.of_head);
-        Item it;
-        walk<true>(a, tl, (uint32_t)(x - (long long)h * line.of_head), &it);
-        const int first = it.b0 + (int)((uint32_t)(x - (long long)h * line.of_head) - it.before);
-        const int last = (int)min((long long)it.b1, first + (x_end - x));
+    Segment seg;
+    for (bool known = false; x < x_end; known = true, x = seg.next) {
+        segment_at(a, tl, line, x, x_end, known, &seg);
+        const Item& it = seg.it;
+        const int h = seg.h, first = seg.first, last = seg.last;
+        if (first == last) continue;                       // (the share ends among the places in front)
         const bool whole = first == it.b0 && last == it.b1;
 
         // this lane's query row
@@ -438,47 +452,47 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const float l = over_halves_sum(st.l);
         if (whole) store_rows(a, st, l, it.rows.q0 + i, head, wave * 32 + (lane & 31) < tile_rows);
         else {
-            store_part(parts + (2ll * share + (x > share * line.share ? 1 : 0)) * kPartFloats, st, l);
+            store_part(parts + (2ll * share + slot_of(blocks_from(it, tl, line, h), share, line.share)) * kPartFloats, st, l);
             if (last < it.b1) cut = cut_of(it, tl, line, share, h);
         }
-        x += last - first;
     }
     if (threadIdx.x == 0) cuts[share] = cut;
 }
 
-// One wave a cut and 32 rows.
+// One wave a cut, 32 rows and 32 dims.
 __global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a, int group, const float* parts, const Cut* cuts)
 {
-    const int share = blockIdx.x >> 3, wave = blockIdx.x & 7, lane = threadIdx.x;
+    const int share = blockIdx.x >> 5, wave = (blockIdx.x >> 2) & 7, d = blockIdx.x & 3, lane = threadIdx.x, half = lane >> 5;
     const Cut c = cuts[share];
     if (c.parts == 0 || wave * 32 >= c.rows) return;
     auto part = [&](int g) { return parts + (2ll * (share + g) + (g == 0 ? c.slot : 0)) * kPartFloats; };
     const int at_m = kRows * kHeadDim + wave * 32 + (lane & 31);
-    Softmax st;
-    st.m = -INFINITY;
-    for (int g = 0; g < c.parts; ++g) st.m = fmaxf(st.m, part(g)[at_m]);
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int g = 0; g < c.parts; ++g) m = fmaxf(m, part(g)[at_m]);
+    const float ms = m == -INFINITY ? 0.f : m;
     float l = 0.f;
+    f32x4 o[4];
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) st.o[d][j] = 0.f;
+    for (int j = 0; j < 4; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int g = 0; g < c.parts; ++g) {
         const float* p = part(g);
-        const float m = p[at_m];
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - st.m);
+        const float f = __builtin_amdgcn_exp2f(p[at_m] - ms);
         l = fmaf(p[at_m + kRows], f, l);
-        const f32x4* o = reinterpret_cast<const f32x4*>(p) + wave * 16 * 64 + lane;
+        const f32x4* from = reinterpret_cast<const f32x4*>(p) + (wave * 16 + 4 * d) * 64 + lane;
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int j = 0; j < 4; ++j) {
+            const f32x4 w = from[j * 64];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x4 w = o[(4 * d + j) * 64];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) st.o[d][4 * j + e] = fmaf(w[e], f, st.o[d][4 * j + e]);
-            }
+            for (int e = 0; e < 4; ++e) o[j][e] = fmaf(w[e], f, o[j][e]);
+        }
     }
-    const int r = min(wave * 32 + (lane & 31), c.rows - 1);
-    store_rows(a, st, l, c.q0 + r / group, c.head * group + r % group, wave * 32 + (lane & 31) < c.rows);
+    const int r = wave * 32 + (lane & 31);
+    if (r >= c.rows) return;
+    const long long row = (long long)(c.q0 + r / group) * a.n_q_heads + c.head * group + r % group;
+    store_dims(a, row, d, half, o, l);
+    if (a.lse && d == 0 && half == 0) a.lse[row] = lse_of(m, l);
 }
 
 Tiling chunk_tiling(int group, int over)
@@ -489,7 +503,8 @@ Tiling chunk_tiling(int group, int over)
     t.over = over;
     t.most = 0x7fffffff;
     t.unit = kKeys;
-    t.least = 4;
+    t.ahead = 3;
+    t.least = 4 + t.ahead;
     t.workgroups = kWorkgroups;
     return t;
 }
@@ -509,7 +524,7 @@ hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, h
     hipLaunchKernelGGL(kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(8 * kWorkgroups), dim3(64), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
+    hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(32 * kWorkgroups), dim3(64), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
     return hipGetLastError();
 }
 

@@ -3,7 +3,8 @@
 // A sequence's query rows of one KV head are its new tokens times the G heads of the group, token after token.  An item is a tile of such rows
 // with the blocks of keys that some of them attend.  All items' blocks, head after head, sequence after sequence, are one line that is cut into equal
 // shares, a workgroup each: lengths are known on the device only, and one long sequence among short ones, or few rows over many keys,
-// come out even.  An item within a share is finished there; one that is cut leaves its parts (maximum, sum and weighted values, in fp32) in the
+// come out even.  In front of its blocks an item has some places that stand for its beginning and end (the first loads, the results), so that shares of
+// many short items do not take longer.  An item within a share is finished there; one that is cut leaves its parts (maximum, sum and weighted values, in fp32) in the
 // workspace for the launch behind.
 #pragma once
 #include "mp_device.h"
@@ -19,7 +20,8 @@ struct Tiling {
     int tokens;               // of a tile
     int over, most;
     int unit;                 // keys of a block
-    int least;                // blocks of a share, at least
+    int ahead;                // places in front of an item's blocks
+    int least;                // places of a share, at least
     int workgroups;
 };
 
@@ -41,7 +43,7 @@ struct Item {
     int b, tile;
     SequenceRows rows;
     int b0, b1;               // its blocks
-    uint32_t before;          // blocks of the items before it (of one head)
+    uint32_t before;          // places of the items before it (of one head)
 };
 
 __device__ __forceinline__ int room_of(const PagedAttention& a) { return a.c.table_stride << a.c.page_shift; }
@@ -54,7 +56,7 @@ __device__ __forceinline__ void blocks_of_tile(const PagedAttention& a, const Ti
 
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
-// Blocks of one head's items in all; kFind: up to the item that block x of the line lies in, which goes to *found.  One wave, 64 sequences (or,
+// Places of one head's items in all; kFind: up to the item that place x of the line lies in, which goes to *found.  One wave, 64 sequences (or,
 // where some have several tiles, 64 tiles) at a time.
 template <bool kFind>
 __device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, uint32_t x, Item* found)
@@ -86,7 +88,7 @@ __device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, uint32_t x, 
             }
             int b0 = 0, b1 = 0;
             if (there) blocks_of_tile(a, tl, m, tile, &b0, &b1);
-            const uint32_t incl = wave_incl_scan_u32((uint32_t)(b1 - b0));
+            const uint32_t incl = wave_incl_scan_u32(there ? (uint32_t)(tl.ahead + b1 - b0) : 0u);
             if constexpr (kFind) {
                 const unsigned long long past = __ballot(sum + incl > x);
                 if (past) {
@@ -98,7 +100,7 @@ __device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, uint32_t x, 
                     found->rows.base = lane_value(m.base, at);
                     found->b0 = lane_value(b0, at);
                     found->b1 = lane_value(b1, at);
-                    found->before = sum + (uint32_t)lane_value((int)incl, at) - (uint32_t)(found->b1 - found->b0);
+                    found->before = sum + (uint32_t)lane_value((int)incl, at) - (uint32_t)(tl.ahead + found->b1 - found->b0);
                     return sum;
                 }
             }
@@ -131,6 +133,33 @@ __device__ __forceinline__ int share_of(const Line& l, int block)
     return 8 * of_xcd + (i - of_xcd) * 8 + xcd;
 }
 
+// Where the line is at a place of it: the item, and the blocks of it that lie between that place and `end`.
+struct Segment {
+    Item it;
+    int h, first, last;
+    long long next;           // place behind it
+};
+__device__ __forceinline__ long long blocks_from(const Item& it, const Tiling& tl, const Line& line, int h)
+{
+    return (long long)h * line.of_head + it.before + tl.ahead;
+}
+// `known`: s->it is the item before, which ended at x.
+__device__ __forceinline__ void segment_at(const PagedAttention& a, const Tiling& tl, const Line& line, long long x, long long end, bool known, Segment* s)
+{
+    Item& it = s->it;
+    if (known && (it.tile + 1) * tl.tokens < it.rows.n) {
+        it.before += (uint32_t)(tl.ahead + it.b1 - it.b0);
+        blocks_of_tile(a, tl, it.rows, ++it.tile, &it.b0, &it.b1);
+    } else {
+        s->h = (int)(x / line.of_head);
+        walk<true>(a, tl, (uint32_t)(x - (long long)s->h * line.of_head), &it);
+    }
+    const long long x0 = blocks_from(it, tl, line, s->h), x1 = x0 + (it.b1 - it.b0);
+    s->next = min(x1, end);
+    s->first = it.b0 + (int)max(x - x0, 0ll);
+    s->last = it.b0 + (int)max(s->next - x0, 0ll);
+}
+
 // An item that begins in a workgroup's share and ends in another one's, for the launch that puts its parts together: a line for each
 // workgroup, written by it (parts == 0: none).
 struct Cut {
@@ -141,7 +170,7 @@ struct Cut {
 };
 __device__ __forceinline__ Cut cut_of(const Item& it, const Tiling& tl, const Line& line, int share, int h)
 {
-    const long long x0 = (long long)h * line.of_head + it.before;
+    const long long x0 = blocks_from(it, tl, line, h);
     const Parts p = parts_of(x0, x0 + (it.b1 - it.b0), line.share);
     Cut c{};
     c.parts = p.first == share ? (int)(p.last - p.first) + 1 : 0;

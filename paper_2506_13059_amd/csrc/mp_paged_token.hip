@@ -255,12 +255,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
     long long x = share * line.share;
     const long long x_end = min(x + line.share, line.all);
     Cut cut{};
-    while (x < x_end) {
-        const int h = (int)(x / line.of_head);
-        Item it;
-        walk<true>(a, tl, (uint32_t)(x - (long long)h * line.of_head), &it);
-        const int first = it.b0 + (int)((uint32_t)(x - (long long)h * line.of_head) - it.before);
-        const int last = (int)min((long long)it.b1, first + (x_end - x));
+    Segment seg;
+    for (bool known = false; x < x_end; known = true, x = seg.next) {
+        segment_at(a, tl, line, x, x_end, known, &seg);
+        const Item& it = seg.it;
+        const int h = seg.h, first = seg.first, last = seg.last;
+        if (first == last) continue;                       // (the share ends among the places in front)
         const bool whole = first == it.b0 && last == it.b1;
         const int tile_rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * G;
         const int r = min(col, tile_rows - 1);
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
             f[w] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_m[w * 16 + col] - M);
             L = fmaf(sm_l[w * 16 + col], f[w], L);
         }
-        float* part = parts + (2ll * share + (x > share * line.share ? 1 : 0)) * kPartFloats;
+        float* part = parts + (2ll * share + slot_of(blocks_from(it, tl, line, h), share, line.share)) * kPartFloats;
 #pragma unroll
         for (int dd = 0; dd < 2; ++dd) {
             const int d = wave + 4 * dd;
@@ -339,7 +339,6 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
             if (last < it.b1) cut = cut_of(it, tl, line, share, h);
         }
         __syncthreads();
-        x += last - first;
     }
     if (threadIdx.x == 0) cuts[share] = cut;
 }
@@ -397,7 +396,8 @@ hipError_t launch_paged_tokens(const PagedAttention& a, float* room, hipStream_t
     tl.over = 0;
     tl.most = kPagedTokenRows;
     tl.unit = kWaves * kTile;
-    tl.least = 1;
+    tl.ahead = 2;
+    tl.least = 1 + tl.ahead;
     tl.workgroups = kWorkgroups;
     Cut* cuts = reinterpret_cast<Cut*>(room);
     float* parts = room + kCutFloats;
