@@ -26,7 +26,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 
 # mp_assign.hip: keep the MFMA accumulators in ordinary vector registers; the comparison code reads
 # every one of them, and copying them out of accumulation registers costs an instruction each
-EXTRA_FLAGS = {"mp_assign.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# mp_paged_token.hip: the same; its 64-row kernel copied the accumulators back and forth, 500 instructions a tile
+EXTRA_FLAGS = {"mp_assign.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "mp_paged_token.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _headers():

@@ -48,9 +48,9 @@ struct PagedAttention {
     float* partials;
 };
 size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_seqs, int max_new);
-constexpr int kPagedTokenRows = 16;      // query rows a KV head that the kernel for single tokens takes
-size_t paged_token_floats();
-hipError_t launch_paged_tokens(const PagedAttention& a, float* room, hipStream_t s);                // sequences of up to that many
+// The kernel for few tokens: sequences of up to `rows` query rows a KV head (16, 32 or 64).
+size_t paged_token_floats(int rows);
+hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s);
 size_t paged_chunk_floats();
 hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s);     // sequences of more than `over` query rows a head
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s);

@@ -10,15 +10,19 @@ namespace mp {
 
 namespace {
 
-// Which kernels a call runs: those for single tokens take sequences of few query rows, those for chunks the others, or all where no sequence need
-// have few (there is one, or the call's tokens are as many as its sequences can have).
+// Which kernels a call runs.  That for few tokens takes sequences of up to `tokens` query rows a KV head (0: it does not run): as many as any sequence can
+// have, where it can.  Otherwise that for chunks runs, and the former takes the sequences of up to 16 rows, unless none need be there (one sequence, or as many tokens in the call
+// as its sequences can have).
 struct Kernels {
-    bool tokens, chunks;
+    int tokens;
+    bool chunks;
 };
 Kernels kernels_of(int n_tokens, int group, int n_seqs, int max_new)
 {
-    if ((long long)max_new * group <= kPagedTokenRows) return Kernels{true, false};
-    return Kernels{n_seqs > 1 && (long long)n_seqs * max_new > n_tokens, true};
+    const long long rows = (long long)max_new * group;
+    for (int most = 16; most <= 64; most *= 2)
+        if (rows <= most) return Kernels{most, false};
+    return Kernels{n_seqs > 1 && (long long)n_seqs * max_new > n_tokens ? 16 : 0, true};
 }
 
 }  // namespace
@@ -27,7 +31,7 @@ size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_s
 {
     if (n_tokens <= 0 || n_seqs <= 0) return 0;
     const Kernels k = kernels_of(n_tokens, n_q_heads / n_kv_heads, n_seqs, max_new);
-    return (k.tokens ? paged_token_floats() : 0) + (k.chunks ? paged_chunk_floats() : 0);
+    return (k.tokens ? paged_token_floats(k.tokens) : 0) + (k.chunks ? paged_chunk_floats() : 0);
 }
 
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s)
@@ -36,11 +40,11 @@ hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s)
     const Kernels k = kernels_of(a.n_tokens, a.n_q_heads / a.c.n_kv, a.c.n_seqs, a.max_new);
     float* room = a.partials;
     if (k.tokens) {
-        const hipError_t e = launch_paged_tokens(a, room, s);
+        const hipError_t e = launch_paged_tokens(a, k.tokens, room, s);
         if (e != hipSuccess) return e;
-        room += paged_token_floats();
+        room += paged_token_floats(k.tokens);
     }
-    return k.chunks ? launch_paged_chunks(a, k.tokens ? kPagedTokenRows : 0, room, s) : hipSuccess;
+    return k.chunks ? launch_paged_chunks(a, k.tokens, room, s) : hipSuccess;
 }
 
 }  // namespace mp

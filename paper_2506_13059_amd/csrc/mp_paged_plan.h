@@ -39,6 +39,13 @@ __device__ __forceinline__ SequenceRows rows_of_sequence(const PagedAttention& a
     return r;
 }
 
+// Of sequence s0 + lane.
+__device__ __forceinline__ SequenceRows rows_of_lane(const PagedAttention& a, int s0)
+{
+    const int b = s0 + (threadIdx.x & 63);
+    return b < a.c.n_seqs ? rows_of_sequence(a, b) : SequenceRows{0, 0, 0};
+}
+
 struct Item {
     int b, tile;
     SequenceRows rows;
@@ -58,14 +65,14 @@ __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_am
 
 // Places of one head's items in all; kFind: up to the item that place x of the line lies in, which goes to *found.  One wave, 64 sequences (or,
 // where some have several tiles, 64 tiles) at a time.
+// `head`: rows_of_lane(a, 0).
 template <bool kFind>
-__device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, uint32_t x, Item* found)
+__device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const SequenceRows& head, uint32_t x, Item* found)
 {
     const int lane = threadIdx.x & 63;
     uint32_t sum = 0;
     for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
-        SequenceRows r{0, 0, 0};
-        if (s0 + lane < a.c.n_seqs) r = rows_of_sequence(a, s0 + lane);
+        const SequenceRows r = s0 == 0 ? head : rows_of_lane(a, s0);
         const long long rows = (long long)r.n * tl.group;
         const int tiles = rows > tl.over && rows <= tl.most ? (r.n + tl.tokens - 1) / tl.tokens : 0;
         const bool several = __any(tiles > 1);
@@ -112,6 +119,7 @@ __device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, uint32_t x, 
 
 // The line and its shares.  Neighbouring shares go to workgroups of one XCD: they mostly work on one head, whose keys its L2 then holds once.
 struct Line {
+    SequenceRows head;        // the lane's among the first 64 sequences: walks begin with them, and need not ask for them again
     uint32_t of_head;
     long long all, share;
     int used;                 // workgroups with a share
@@ -119,7 +127,8 @@ struct Line {
 __device__ __forceinline__ Line line_of(const PagedAttention& a, const Tiling& tl)
 {
     Line l;
-    l.of_head = walk<false>(a, tl, 0, nullptr);
+    l.head = rows_of_lane(a, 0);
+    l.of_head = walk<false>(a, tl, l.head, 0, nullptr);
     l.all = (long long)l.of_head * a.c.n_kv;
     l.share = max((l.all + tl.workgroups - 1) / tl.workgroups, (long long)tl.least);
     l.used = (int)((l.all + l.share - 1) / l.share);
@@ -152,7 +161,7 @@ __device__ __forceinline__ void segment_at(const PagedAttention& a, const Tiling
         blocks_of_tile(a, tl, it.rows, ++it.tile, &it.b0, &it.b1);
     } else {
         s->h = (int)(x / line.of_head);
-        walk<true>(a, tl, (uint32_t)(x - (long long)s->h * line.of_head), &it);
+        walk<true>(a, tl, line.head, (uint32_t)(x - (long long)s->h * line.of_head), &it);
     }
     const long long x0 = blocks_from(it, tl, line, s->h), x1 = x0 + (it.b1 - it.b0);
     s->next = min(x1, end);

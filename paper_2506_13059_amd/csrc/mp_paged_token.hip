@@ -1,9 +1,9 @@
 // Attention of one or a few new tokens over a paged cache, on the matrix cores, for gfx950.  (mp_paged_attn.hip says what is computed.)
 //
-// Up to 16 query rows (new tokens times the heads of a group) meet every key of their sequence once: bound by memory.  A wave streams tiles of
+// Up to 64 query rows (new tokens times the heads of a group; kGroups times 16) meet every key of their sequence once: bound by memory.  A wave streams tiles of
 // 32 keys and values straight to LDS (global_load_lds, 16 bytes a lane, four rows an instruction) into a ring of two tiles, three of four
-// 8 KiB pieces on their way while one is used.  S^T = K Q^T is eight v_mfma_f32_16x16x32_bf16 and O^T += V^T P^T as many: a lane holds one
-// query row (its column) in both, and what it holds of S^T is what the second product takes of it.  Four waves with runs of tiles of their own make a workgroup,
+// 8 KiB pieces on their way while one is used.  For 16 rows, S^T = K Q^T is eight v_mfma_f32_16x16x32_bf16 and O^T += V^T P^T as many: a lane holds one
+// query row of each 16 (its column) in both, and what it holds of S^T is what the second product takes of it.  Four waves with runs of tiles of their own make a workgroup,
 // whose sums meet in LDS; workgroups have equal shares of all sequences' keys (mp_paged_plan.h).
 #include <type_traits>
 
@@ -20,10 +20,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
-constexpr int kWaves = 4, kTile = 32, kRows = 16;
+constexpr int kWaves = 4, kTile = 32;
 constexpr int kPiece = kTile * 256, kSlot = 2 * kPiece, kRing = 2 * kSlot;
 constexpr int kWorkgroups = 256;
-constexpr int kPartFloats = kRows * kHeadDim + 2 * kRows;       // a part: weighted values as the lanes hold them, then maxima, then sums
+// A part: weighted values as the lanes hold them, then maxima, then sums.
+constexpr int part_floats(int groups) { return 16 * groups * kHeadDim + 2 * 16 * groups; }
 constexpr size_t kCutFloats = sizeof(Cut) / sizeof(float) * kWorkgroups;
 
 __device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds_off)
@@ -38,9 +39,10 @@ __device__ __forceinline__ void wait_vm()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+template <int kGroups>
 struct State {
-    f32x4 o[8];              // of this lane's query row: dims 16 d + 4 (lane / 16) + i
-    float m, l;              // m in powers of two; l of the keys that the lane has seen
+    f32x4 o[kGroups][8];     // of this lane's query rows (one of each 16): dims 16 d + 4 (lane / 16) + i
+    float m[kGroups], l[kGroups];      // m in powers of two; l of the keys that the lane has seen
 };
 
 struct Source {
@@ -50,8 +52,10 @@ struct Source {
 };
 
 // Tiles [t0, t1) of 32 keys through one wave; `ring`: LDS offset of its ring.
-__device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 (&q)[4], int t0, int t1, uint32_t ring, int position, int pos_min, int pos_max,
-                                       int window, float scale)
+// kOnePage: pages of 32 rows or more, which hold whole tiles, so that a tile's address is a scalar.
+template <int kGroups, bool kOnePage>
+__device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, const bf16x8 (&q)[kGroups][4], int t0, int t1, uint32_t ring,
+                                       const int (&position)[kGroups], int pos_min, int pos_max, int window, float scale)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     // LDS: chunk j (16 bytes) of key r lies at j ^ r % 16, of value r at j ^ 2 (r % 8): the lanes of a read touch different banks
@@ -60,15 +64,25 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
     const uint32_t v_at = ring + kPiece + (uint32_t)(vr * 256 + ((((col & 3) >> 1) ^ ((vr & 7) << 1)) << 4) + (col & 1) * 8);      // ^ 32 d
 
     // (entries are looked at two tiles after they were asked for: looked at at once, they made the wave wait for all loads before them)
-    auto entry_at = [&](int t) { return c.entries[min(t * kTile + (lane & 31), c.end - 1) >> c.shift]; };      // of key 32 t + lane % 32
-    auto held = [&](int t, int entry) { return (uint32_t)__ballot(t * kTile + (lane & 31) < c.end && (uint32_t)entry < (uint32_t)c.n_pages); };
-    long long off[8];
-    auto offsets = [&](int t, int entry, uint32_t valid) {    // bytes, of rows 4 i + g; those that are not there: somewhere in page 0
-        if (c.shift >= 5) {                  // (the tile lies in one page)
-            const int page = valid ? __builtin_amdgcn_readfirstlane(entry) : 0;
-            const long long at = row_of(page, c.h, c.n_kv, c.shift, t * kTile) * 256 + g * 256;
+    auto entry_at = [&](int t) { return c.entries[min(t * kTile + (kOnePage ? 0 : lane & 31), c.end - 1) >> c.shift]; };      // of key 32 t (+ lane % 32)
+    auto held = [&](int t, int entry) {
+        if constexpr (kOnePage) {
+            const int n = c.end - t * kTile;
+            return (uint32_t)__builtin_amdgcn_readfirstlane(entry) < (uint32_t)c.n_pages ? n >= 32 ? ~0u : (1u << n) - 1u : 0u;
+        } else {
+            return (uint32_t)__ballot(t * kTile + (lane & 31) < c.end && (uint32_t)entry < (uint32_t)c.n_pages);
+        }
+    };
+    // What a lane loads, in bytes from a tile's first row: rows 4 i + g, i = 0 .. 3 (of keys; 4 .. 7 are 4096 on) or 0, 1 (of values; 2 and on are 2048 on).
+    uint32_t k_from[4], v_from[2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) off[i] = at + i * 1024;
+    for (int i = 0; i < 4; ++i) k_from[i] = (uint32_t)((4 * i + g) * 256 + ((col ^ (4 * i + g)) << 4));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v_from[i] = (uint32_t)((4 * i + g) * 256 + ((col ^ ((4 * i + g) << 1)) << 4));
+    long long off[kOnePage ? 1 : 8];
+    auto offsets = [&](int t, int entry, uint32_t valid) {    // bytes, of the tile or of rows 4 i + g; those that are not there: somewhere in page 0
+        if constexpr (kOnePage) {
+            off[0] = row_of(valid ? __builtin_amdgcn_readfirstlane(entry) : 0, c.h, c.n_kv, c.shift, t * kTile) * 256;
         } else {
             const int mine = (valid >> (lane & 31) & 1) ? entry : 0;
 #pragma unroll
@@ -77,11 +91,19 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
     };
     auto load_keys = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) load_to_lds(c.K + off[i] + ((col ^ ((4 * i + g) & 15)) << 4), ring + (uint32_t)((t & 1) * kSlot + i * 1024));
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t to = ring + (uint32_t)((t & 1) * kSlot + i * 1024);
+            if constexpr (kOnePage) load_to_lds(c.K + off[0] + (i >= 4 ? 4096 : 0) + k_from[i & 3], to);
+            else load_to_lds(c.K + off[i] + (k_from[i & 3] & 255u), to);
+        }
     };
     auto load_values = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) load_to_lds(c.V + off[i] + ((col ^ (((4 * i + g) & 7) << 1)) << 4), ring + (uint32_t)((t & 1) * kSlot + kPiece + i * 1024));
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t to = ring + (uint32_t)((t & 1) * kSlot + kPiece + i * 1024);
+            if constexpr (kOnePage) load_to_lds(c.V + off[0] + (i >> 1) * 2048 + v_from[i & 1], to);
+            else load_to_lds(c.V + off[i] + (v_from[i & 1] & 255u), to);
+        }
     };
 
     // Loads come back in order: K V K V ..., eight instructions a piece, and one for the pages of a tile four ahead now and then; "at most as many on their
@@ -120,48 +142,62 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
             entries[2] = entries[3];
             entries[3] = entry_at(t + 4);
         }
-        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[ks], q[ks], s0, 0, 0, 0);
-            s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[4 + ks], q[ks], s1, 0, 0, 0);
-        }
-        float s[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s[i] = s0[i];
-            s[4 + i] = s1[i];
-        }
         // a tile in which some row sees a key that another one does not
         const bool edge = t * kTile + kTile - 1 > pos_min || (window && t * kTile <= pos_max - window);
-        if (valid != 0xffffffffu || edge) {
-            const int upto = position - t * kTile, from = window ? upto - window : -1;
+        f32x4 s[kGroups][2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int key = 16 * (i >> 2) + 4 * g + (i & 3);
-                s[i] = (valid >> key & 1) && key <= upto && key > from ? s[i] : -INFINITY;
+        for (int r = 0; r < kGroups; ++r) s[r][0] = s[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int r = 0; r < kGroups; ++r) {
+                s[r][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[ks], q[r][ks], s[r][0], 0, 0, 0);
+                s[r][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[4 + ks], q[r][ks], s[r][1], 0, 0, 0);
+            }
+        if (valid != 0xffffffffu || edge) {
+#pragma unroll
+            for (int r = 0; r < kGroups; ++r) {
+                const int upto = position[r] - t * kTile, from = window ? upto - window : -1;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int key = 16 * (i >> 2) + 4 * g + (i & 3);
+                    s[r][i >> 2][i & 3] = (valid >> key & 1) && key <= upto && key > from ? s[r][i >> 2][i & 3] : -INFINITY;
+                }
             }
         }
-        float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]))) * scale;
-        if (__any(mx > st.m)) {              // (the running maximum settles after a few tiles)
-            mx = fmaxf(mx, st.m);
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - mx);
-            st.m = mx;
-            st.l *= f;
+        float mx[kGroups];
+        bool grown = false;
 #pragma unroll
-            for (int d = 0; d < 8; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st.o[d][i] *= f;
+        for (int r = 0; r < kGroups; ++r) {
+            mx[r] = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])), fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3]))) * scale;
+            grown |= mx[r] > st.m[r] + 8.f;
         }
-        const float m = st.m == -INFINITY ? 0.f : st.m;
-        bf16x8 p;
+        // The maximum in use may be up to 2^8 behind: sums in fp32 and products of bf16 have room for it, and it is soon never moved.
+        if (__any(grown)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -m));
-            st.l += e;
-            p[i] = (__bf16)e;
+            for (int r = 0; r < kGroups; ++r) {
+                float n = fmaxf(mx[r], st.m[r]);
+                n = fmaxf(n, __shfl_xor(n, 16, 64));
+                n = fmaxf(n, __shfl_xor(n, 32, 64));
+                const float f = n == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[r] - n);
+                st.m[r] = n;
+                st.l[r] *= f;
+#pragma unroll
+                for (int d = 0; d < 8; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) st.o[r][d][i] *= f;
+            }
+        }
+        bf16x8 p[kGroups];
+#pragma unroll
+        for (int r = 0; r < kGroups; ++r) {
+            const float m = st.m[r] == -INFINITY ? 0.f : st.m[r];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[r][i >> 2][i & 3], scale, -m));
+                st.l[r] += e;
+                p[r][i] = (__bf16)e;
+            }
         }
         wait_vm<kAhead == 2 ? 24 : 16 * kAhead>();
         uint32_t odd = 0;
@@ -203,7 +239,9 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 const auto a = __builtin_shufflevector(v[2 * d], v[2 * d + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-                st.o[4 * d4 + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), p, st.o[4 * d4 + d], 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < kGroups; ++r)
+                    st.o[r][4 * d4 + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), p[r], st.o[r][4 * d4 + d], 0, 0, 0);
             }
         }
         if constexpr (kAhead == 2) load_values(t + 2);
@@ -211,15 +249,18 @@ __device__ __forceinline__ void stream(State& st, const Source& c, const bf16x8 
         for (; odd; odd &= odd - 1) {
             const int key = t * kTile + __builtin_ctz(odd);
             const int page = page_of(c.entries, c.stride, c.n_pages, c.shift, key);
-            const bool sees = key <= position && !(window && key <= position - window);
             const uint2* from = reinterpret_cast<const uint2*>(c.V + row_of(max(page, 0), c.h, c.n_kv, c.shift, key) * 256);
 #pragma unroll
             for (int d = 0; d < 8; ++d) {
                 const uint2 w = from[4 * d + g];
                 const uint32_t u[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (sees && (u[e] & 0x7f800000u) == 0x7f800000u) st.o[d][e] += __uint_as_float(u[e]);
+                for (int r = 0; r < kGroups; ++r) {
+                    const bool sees = key <= position[r] && !(window && key <= position[r] - window);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (sees && (u[e] & 0x7f800000u) == 0x7f800000u) st.o[r][d][e] += __uint_as_float(u[e]);
+                }
             }
         }
     };
@@ -240,9 +281,11 @@ __device__ __forceinline__ void store_row(const PagedAttention& a, int token, in
     if (a.lse && d == 0 && g == 0) a.lse[row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
 }
 
+template <int kGroups, bool kOnePage>
 __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
 {
-    __shared__ __align__(256) unsigned char lds[kWaves * kRing];
+    constexpr int kRows = 16 * kGroups;
+    __shared__ __align__(256) unsigned char lds[kWaves * kRing + 2 * kWaves * kRows * 4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const Line line = line_of(a, tl);
     const int share = share_of(line, blockIdx.x);
@@ -262,15 +305,19 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
         const int h = seg.h, first = seg.first, last = seg.last;
         if (first == last) continue;                       // (the share ends among the places in front)
         const bool whole = first == it.b0 && last == it.b1;
-        const int tile_rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * G;
-        const int r = min(col, tile_rows - 1);
-        const int i = it.tile * tl.tokens + r / G, head = h * G + r % G, position = it.rows.base + i;
-        const int pos_min = lane_value(position, 0), pos_max = lane_value(position, 15);
-        bf16x8 q[4];
-        {
-            const uint4* from = reinterpret_cast<const uint4*>(a.q + (long long)(it.rows.q0 + i) * a.q_stride + (long long)head * kHeadDim);
+        const int tokens = min(it.rows.n - it.tile * tl.tokens, tl.tokens), tile_rows = tokens * G;
+        const int pos_min = it.rows.base + it.tile * tl.tokens, pos_max = pos_min + tokens - 1;
+        int token[kGroups], head[kGroups], position[kGroups];
+        bf16x8 q[kGroups][4];
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) q[ks] = __builtin_bit_cast(bf16x8, from[4 * ks + g]);
+        for (int r = 0; r < kGroups; ++r) {
+            const int row = min(16 * r + col, tile_rows - 1), i = it.tile * tl.tokens + row / G;
+            token[r] = it.rows.q0 + i;
+            head[r] = h * G + row % G;
+            position[r] = it.rows.base + i;
+            const uint4* from = reinterpret_cast<const uint4*>(a.q + (long long)token[r] * a.q_stride + (long long)head[r] * kHeadDim);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) q[r][ks] = __builtin_bit_cast(bf16x8, from[4 * ks + g]);
         }
         Source c;
         c.K = reinterpret_cast<const unsigned char*>(a.c.K);
@@ -284,128 +331,169 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
         c.end = min(pos_max + 1, room_of(a));
         // the wave's tiles: a quarter of the share's
         const int t0 = first * kWaves + wave * (last - first), t1 = min(t0 + (last - first), c.end > 0 ? (c.end - 1) / kTile + 1 : 0);
-        State st;
-        st.m = -INFINITY;
-        st.l = 0.f;
+        State<kGroups> st;
 #pragma unroll
-        for (int d = 0; d < 8; ++d) st.o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (t0 < t1) stream(st, c, q, t0, t1, ring, position, pos_min, pos_max, a.window, a.scale_log2e);
+        for (int r = 0; r < kGroups; ++r) {
+            st.m[r] = -INFINITY;
+            st.l[r] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) st.o[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (t0 < t1) stream<kGroups, kOnePage>(st, c, q, t0, t1, ring, position, pos_min, pos_max, a.window, a.scale_log2e);
 
         // The waves' sums meet.
-        float l = st.l;
-        l += __shfl_xor(l, 16, 64);
-        l += __shfl_xor(l, 32, 64);
         __syncthreads();
-        f32x4* sm_o = reinterpret_cast<f32x4*>(lds);                            // [kWaves][8][64]
-        float* sm_m = reinterpret_cast<float*>(lds + kWaves * 8 * 64 * 16);     // [kWaves][16], then sums
-        float* sm_l = sm_m + kWaves * 16;
+        f32x4* sm_o = reinterpret_cast<f32x4*>(lds);                            // [kWaves][kGroups][8][64]
+        float* sm_m = reinterpret_cast<float*>(lds + kWaves * kRing);           // [kWaves][kRows], then sums
+        float* sm_l = sm_m + kWaves * kRows;
 #pragma unroll
-        for (int d = 0; d < 8; ++d) sm_o[(wave * 8 + d) * 64 + lane] = st.o[d];
-        if (lane < 16) {
-            sm_m[wave * 16 + lane] = st.m;
-            sm_l[wave * 16 + lane] = l;
+        for (int r = 0; r < kGroups; ++r) {
+            float l = st.l[r];
+            l += __shfl_xor(l, 16, 64);
+            l += __shfl_xor(l, 32, 64);
+#pragma unroll
+            for (int d = 0; d < 8; ++d) sm_o[((wave * kGroups + r) * 8 + d) * 64 + lane] = st.o[r][d];
+            if (lane < 16) {
+                sm_m[wave * kRows + 16 * r + lane] = st.m[r];
+                sm_l[wave * kRows + 16 * r + lane] = l;
+            }
         }
         __syncthreads();
-        float M = -INFINITY, L = 0.f, f[kWaves];
+        float* part = parts + (2ll * share + slot_of(blocks_from(it, tl, line, h), share, line.share)) * part_floats(kGroups);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_m[w * 16 + col]);
+        for (int r = 0; r < kGroups; ++r) {
+            float M = -INFINITY, L = 0.f, f[kWaves];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            f[w] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_m[w * 16 + col] - M);
-            L = fmaf(sm_l[w * 16 + col], f[w], L);
-        }
-        float* part = parts + (2ll * share + slot_of(blocks_from(it, tl, line, h), share, line.share)) * kPartFloats;
-#pragma unroll
-        for (int dd = 0; dd < 2; ++dd) {
-            const int d = wave + 4 * dd;
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm_m[w * kRows + 16 * r + col]);
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const f32x4 y = sm_o[(w * 8 + d) * 64 + lane];
+                f[w] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm_m[w * kRows + 16 * r + col] - M);
+                L = fmaf(sm_l[w * kRows + 16 * r + col], f[w], L);
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], f[w], o[e]);
+            for (int dd = 0; dd < 2; ++dd) {
+                const int d = wave + 4 * dd;
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const f32x4 y = sm_o[((w * kGroups + r) * 8 + d) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], f[w], o[e]);
+                }
+                if (whole) {
+                    if (16 * r + col < tile_rows) store_row(a, token[r], head[r], o, M, L, d, g);
+                } else {
+                    reinterpret_cast<f32x4*>(part)[(8 * r + d) * 64 + lane] = o;
+                }
             }
-            if (whole) {
-                if (col < tile_rows) store_row(a, it.rows.q0 + i, head, o, M, L, d, g);
-            } else {
-                reinterpret_cast<f32x4*>(part)[d * 64 + lane] = o;
+            if (!whole && wave == 0 && lane < 16) {
+                part[kRows * kHeadDim + 16 * r + lane] = M;
+                part[kRows * kHeadDim + kRows + 16 * r + lane] = L;
             }
         }
-        if (!whole) {
-            if (threadIdx.x < 16) {
-                part[kRows * kHeadDim + lane] = M;
-                part[kRows * kHeadDim + kRows + lane] = L;
-            }
-            if (last < it.b1) cut = cut_of(it, tl, line, share, h);
-        }
+        if (last < it.b1) cut = cut_of(it, tl, line, share, h);
         __syncthreads();
     }
     if (threadIdx.x == 0) cuts[share] = cut;
 }
 
-// One workgroup a cut and 16 dims: its waves take parts in turn.
+// One workgroup a cut, 16 rows and 16 dims: its waves take parts in turn, eight at a time, so that a cut of up to 32 parts costs one trip to memory.
+template <int kGroups>
 __global__ __launch_bounds__(256) void paged_token_merge_kernel(PagedAttention a, int group, const float* parts, const Cut* cuts)
 {
-    __shared__ float sm[2][16][16];
+    constexpr int kRows = 16 * kGroups;
     __shared__ f32x4 sm_o[4][64];
-    const int share = blockIdx.x >> 3, d = blockIdx.x & 7, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+    __shared__ float sm_m[4][16], sm_l[4][16];
+    const int share = blockIdx.x / (8 * kGroups), r = blockIdx.x / 8 % kGroups, d = blockIdx.x & 7;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const Cut c = cuts[share];
-    if (c.parts == 0) return;
-    auto part = [&](int i) { return parts + (2ll * (share + i) + (i == 0 ? c.slot : 0)) * kPartFloats; };
-    float m = -INFINITY;
-    for (int i = threadIdx.x >> 4; i < c.parts; i += 16) m = fmaxf(m, part(i)[kRows * kHeadDim + col]);
-    sm[0][threadIdx.x >> 4][col] = m;
-    __syncthreads();
-    float M = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) M = fmaxf(M, sm[0][i][col]);
-    const float Ms = M == -INFINITY ? 0.f : M;
-    float l = 0.f;
-    for (int i = threadIdx.x >> 4; i < c.parts; i += 16)
-        l = fmaf(part(i)[kRows * kHeadDim + kRows + col], __builtin_amdgcn_exp2f(part(i)[kRows * kHeadDim + col] - Ms), l);
-    sm[1][threadIdx.x >> 4][col] = l;
+    if (c.parts == 0 || 16 * r >= c.rows) return;
+    float M = -INFINITY, L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = wave; i < c.parts; i += 4) {
-        const float* p = part(i);
-        const float f = __builtin_amdgcn_exp2f(p[kRows * kHeadDim + col] - Ms);
-        const f32x4 y = reinterpret_cast<const f32x4*>(p)[d * 64 + lane];
+    for (int i0 = wave; i0 < c.parts; i0 += 32) {
+        float m[8], l[8];
+        f32x4 y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = min(i0 + 4 * k, c.parts - 1);
+            const float* p = parts + (2ll * (share + i) + (i == 0 ? c.slot : 0)) * part_floats(kGroups);
+            m[k] = p[kRows * kHeadDim + 16 * r + col];
+            l[k] = p[kRows * kHeadDim + kRows + 16 * r + col];
+            y[k] = reinterpret_cast<const f32x4*>(p)[(8 * r + d) * 64 + lane];
+        }
+        float n = M;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (i0 + 4 * k >= c.parts) m[k] = -INFINITY;
+            n = fmaxf(n, m[k]);
+        }
+        const float base = n == -INFINITY ? 0.f : n, before = __builtin_amdgcn_exp2f(M - base);
+        M = n;
+        L *= before;
+        o *= before;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float f = __builtin_amdgcn_exp2f(m[k] - base);
+            if (i0 + 4 * k < c.parts) {
+                L = fmaf(l[k], f, L);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(y[k][e], f, o[e]);
+            }
+        }
+    }
+    sm_o[wave][lane] = o;
+    if (lane < 16) {
+        sm_m[wave][lane] = M;
+        sm_l[wave][lane] = L;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) M = fmaxf(M, sm_m[w][col]);
+    const float base = M == -INFINITY ? 0.f : M;
+    L = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sm_m[w][col] - base);
+        L = fmaf(sm_l[w][col], f, L);
+        const f32x4 y = sm_o[w][lane];
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], f, o[e]);
     }
-    sm_o[wave][lane] = o;
-    __syncthreads();
-    if (wave != 0) return;
-    float L = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) L += sm[1][i][col];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) o += sm_o[w][lane];
-    if (col < c.rows) store_row(a, c.q0 + col / group, c.head * group + col % group, o, M, L, d, g);
+    const int row = 16 * r + col;
+    if (row < c.rows) store_row(a, c.q0 + row / group, c.head * group + row % group, o, M, L, d, g);
 }
 
-}  // namespace
-
-size_t paged_token_floats() { return (size_t)2 * kWorkgroups * kPartFloats + kCutFloats; }
-
-hipError_t launch_paged_tokens(const PagedAttention& a, float* room, hipStream_t s)
+template <int kGroups>
+hipError_t launch(const PagedAttention& a, float* room, hipStream_t s)
 {
     Tiling tl;
     tl.group = a.n_q_heads / a.c.n_kv;
-    tl.tokens = kRows / tl.group;
+    tl.tokens = 16 * kGroups / tl.group;
     tl.over = 0;
-    tl.most = kPagedTokenRows;
+    tl.most = 16 * kGroups;
     tl.unit = kWaves * kTile;
     tl.ahead = 2;
     tl.least = 1 + tl.ahead;
     tl.workgroups = kWorkgroups;
     Cut* cuts = reinterpret_cast<Cut*>(room);
     float* parts = room + kCutFloats;
-    hipLaunchKernelGGL(paged_token_kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
+    const auto kernel = a.c.page_shift >= 5 ? paged_token_kernel<kGroups, true> : paged_token_kernel<kGroups, false>;
+    hipLaunchKernelGGL(kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_token_merge_kernel, dim3(8 * kWorkgroups), dim3(256), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
+    hipLaunchKernelGGL((paged_token_merge_kernel<kGroups>), dim3(8 * kGroups * kWorkgroups), dim3(256), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
     return hipGetLastError();
+}
+
+}  // namespace
+
+size_t paged_token_floats(int rows) { return (size_t)2 * kWorkgroups * part_floats(rows / 16) + kCutFloats; }
+
+hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s)
+{
+    return rows == 16 ? launch<1>(a, room, s) : rows == 32 ? launch<2>(a, room, s) : rows == 64 ? launch<4>(a, room, s) : hipErrorInvalidValue;
 }
 
 }  // namespace mp
