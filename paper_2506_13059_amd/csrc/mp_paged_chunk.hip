@@ -21,7 +21,6 @@ typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
 constexpr int kWaves = 8, kKeys = 64, kRows = 32 * kWaves;
 constexpr int kRing = 4, kPiece = kKeys * 256, kBlockBytes = 2 * kPiece;      // LDS: blocks, keys and then values of one
-constexpr int kWorkgroups = 256;
 constexpr int kPartFloats = kRows * kHeadDim + 2 * kRows;       // a part: weighted values as the lanes hold them, then maxima, then sums
 
 __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(lds_byte*)p; }
@@ -200,7 +199,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         // this lane's query row
         const int tile_rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * G;
         const int r = min(wave * 32 + (lane & 31), tile_rows - 1);
-        const int i = it.tile * tl.tokens + r / G, head = h * G + r % G;
+        const int in_tile = token_of_row(tl, r), i = it.tile * tl.tokens + in_tile, head = h * G + r - in_tile * G;
         const int position = it.rows.base + i;
         const bool active = wave * 32 < tile_rows;
         const int pos_min = lane_value(position, 0), pos_max = lane_value(position, 31);
@@ -452,7 +451,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const float l = over_halves_sum(st.l);
         if (whole) store_rows(a, st, l, it.rows.q0 + i, head, wave * 32 + (lane & 31) < tile_rows);
         else {
-            store_part(parts + (2ll * share + slot_of(blocks_from(it, tl, line, h), share, line.share)) * kPartFloats, st, l);
+            store_part(parts + (2ll * share + slot_of(blocks_from(it, line, h), share, line.share)) * kPartFloats, st, l);
             if (last < it.b1) cut = cut_of(it, tl, line, share, h);
         }
     }
@@ -495,20 +494,6 @@ __global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a,
     if (a.lse && d == 0 && half == 0) a.lse[row] = lse_of(m, l);
 }
 
-Tiling chunk_tiling(int group, int over)
-{
-    Tiling t;
-    t.group = group;
-    t.tokens = kRows / group;
-    t.over = over;
-    t.most = 0x7fffffff;
-    t.unit = kKeys;
-    t.ahead = 3;
-    t.least = 4 + t.ahead;
-    t.workgroups = kWorkgroups;
-    return t;
-}
-
 constexpr size_t kCutFloats = sizeof(Cut) / sizeof(float) * kWorkgroups;
 
 }  // namespace
@@ -517,7 +502,7 @@ size_t paged_chunk_floats() { return (size_t)2 * kWorkgroups * kPartFloats + kCu
 
 hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s)
 {
-    const Tiling tl = chunk_tiling(a.n_q_heads / a.c.n_kv, over);
+    const Tiling tl = tiling(a.n_q_heads / a.c.n_kv, kRows, over, 0x7fffffff, kKeys, 3, 4);
     Cut* cuts = reinterpret_cast<Cut*>(room);
     float* parts = room + kCutFloats;
     const auto kernel = a.c.page_shift >= 3 ? paged_chunk_kernel<true> : paged_chunk_kernel<false>;

@@ -22,8 +22,14 @@ struct Tiling {
     int unit;                 // keys of a block
     int ahead;                // places in front of an item's blocks
     int least;                // places of a share, at least
-    int workgroups;
+    int inverse;              // row / group = row * inverse >> 16 for the rows of a tile
 };
+constexpr int kWorkgroups = 256;
+inline Tiling tiling(int group, int rows, int over, int most, int unit, int ahead, int least)
+{
+    return Tiling{group, rows / group, over, most, unit, ahead, least, 65536 / group + 1};
+}
+__device__ __forceinline__ int token_of_row(const Tiling& tl, int row) { return row * tl.inverse >> 16; }
 
 struct SequenceRows {
     int q0, n, base;          // first token, tokens, position of the first
@@ -63,11 +69,10 @@ __device__ __forceinline__ void blocks_of_tile(const PagedAttention& a, const Ti
 
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
-// Places of one head's items in all; kFind: up to the item that place x of the line lies in, which goes to *found.  One wave, 64 sequences (or,
-// where some have several tiles, 64 tiles) at a time.
-// `head`: rows_of_lane(a, 0).
+// Places of one head's items in all, `ahead` of them in front of each one's blocks (*items: how many there are); kFind: up to the item that place x of the line
+// lies in, which goes to *found.  One wave, 64 sequences (or, where some have several tiles, 64 tiles) at a time.  `head`: rows_of_lane(a, 0).
 template <bool kFind>
-__device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const SequenceRows& head, uint32_t x, Item* found)
+__device__ __forceinline__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const SequenceRows& head, int ahead, uint32_t x, Item* found, uint32_t* items)
 {
     const int lane = threadIdx.x & 63;
     uint32_t sum = 0;
@@ -95,7 +100,8 @@ __device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const Sequen
             }
             int b0 = 0, b1 = 0;
             if (there) blocks_of_tile(a, tl, m, tile, &b0, &b1);
-            const uint32_t incl = wave_incl_scan_u32(there ? (uint32_t)(tl.ahead + b1 - b0) : 0u);
+            const uint32_t incl = wave_incl_scan_u32(there ? (uint32_t)(ahead + b1 - b0) : 0u);
+            if constexpr (!kFind) *items += (uint32_t)__popcll(__ballot(there));
             if constexpr (kFind) {
                 const unsigned long long past = __ballot(sum + incl > x);
                 if (past) {
@@ -107,7 +113,7 @@ __device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const Sequen
                     found->rows.base = lane_value(m.base, at);
                     found->b0 = lane_value(b0, at);
                     found->b1 = lane_value(b1, at);
-                    found->before = sum + (uint32_t)lane_value((int)incl, at) - (uint32_t)(tl.ahead + found->b1 - found->b0);
+                    found->before = sum + (uint32_t)lane_value((int)incl, at) - (uint32_t)(ahead + found->b1 - found->b0);
                     return sum;
                 }
             }
@@ -121,20 +127,30 @@ __device__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const Sequen
 struct Line {
     SequenceRows head;        // the lane's among the first 64 sequences: walks begin with them, and need not ask for them again
     uint32_t of_head;
+    int ahead;
     long long all, share;
     int used;                 // workgroups with a share
 };
+// x / d (a line of 2^32 places or more is possible in principle only)
+__device__ __forceinline__ long long quotient(long long x, long long d)
+{
+    return ((x | d) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;
+}
 __device__ __forceinline__ Line line_of(const PagedAttention& a, const Tiling& tl)
 {
     Line l;
     l.head = rows_of_lane(a, 0);
-    l.of_head = walk<false>(a, tl, l.head, 0, nullptr);
+    uint32_t items = 0;
+    l.of_head = walk<false>(a, tl, l.head, 0, 0, nullptr, &items);
+    // (where shares are a few blocks anyway, every workgroup is worth more than evenness)
+    l.ahead = (long long)l.of_head * a.c.n_kv >= 8 * kWorkgroups ? tl.ahead : 0;
+    l.of_head += (uint32_t)l.ahead * items;
     l.all = (long long)l.of_head * a.c.n_kv;
-    l.share = max((l.all + tl.workgroups - 1) / tl.workgroups, (long long)tl.least);
-    l.used = (int)((l.all + l.share - 1) / l.share);
+    l.share = max((l.all + kWorkgroups - 1) / kWorkgroups, (long long)(tl.least + l.ahead));
+    l.used = (int)quotient(l.all + l.share - 1, l.share);
     return l;
 }
-// The share of a workgroup (of tl.workgroups); those from l.used on are empty.
+// The share of a workgroup; those from l.used on are empty.
 __device__ __forceinline__ int share_of(const Line& l, int block)
 {
     const int of_xcd = (l.used + 7) >> 3, xcd = block & 7, i = block >> 3;
@@ -148,22 +164,22 @@ struct Segment {
     int h, first, last;
     long long next;           // place behind it
 };
-__device__ __forceinline__ long long blocks_from(const Item& it, const Tiling& tl, const Line& line, int h)
+__device__ __forceinline__ long long blocks_from(const Item& it, const Line& line, int h)
 {
-    return (long long)h * line.of_head + it.before + tl.ahead;
+    return (long long)h * line.of_head + it.before + line.ahead;
 }
 // `known`: s->it is the item before, which ended at x.
 __device__ __forceinline__ void segment_at(const PagedAttention& a, const Tiling& tl, const Line& line, long long x, long long end, bool known, Segment* s)
 {
     Item& it = s->it;
     if (known && (it.tile + 1) * tl.tokens < it.rows.n) {
-        it.before += (uint32_t)(tl.ahead + it.b1 - it.b0);
+        it.before += (uint32_t)(line.ahead + it.b1 - it.b0);
         blocks_of_tile(a, tl, it.rows, ++it.tile, &it.b0, &it.b1);
     } else {
-        s->h = (int)(x / line.of_head);
-        walk<true>(a, tl, line.head, (uint32_t)(x - (long long)s->h * line.of_head), &it);
+        s->h = (int)quotient(x, line.of_head);
+        walk<true>(a, tl, line.head, line.ahead, (uint32_t)(x - (long long)s->h * line.of_head), &it, nullptr);
     }
-    const long long x0 = blocks_from(it, tl, line, s->h), x1 = x0 + (it.b1 - it.b0);
+    const long long x0 = blocks_from(it, line, s->h), x1 = x0 + (it.b1 - it.b0);
     s->next = min(x1, end);
     s->first = it.b0 + (int)max(x - x0, 0ll);
     s->last = it.b0 + (int)max(s->next - x0, 0ll);
@@ -179,7 +195,7 @@ struct Cut {
 };
 __device__ __forceinline__ Cut cut_of(const Item& it, const Tiling& tl, const Line& line, int share, int h)
 {
-    const long long x0 = blocks_from(it, tl, line, h);
+    const long long x0 = blocks_from(it, line, h);
     const Parts p = parts_of(x0, x0 + (it.b1 - it.b0), line.share);
     Cut c{};
     c.parts = p.first == share ? (int)(p.last - p.first) + 1 : 0;

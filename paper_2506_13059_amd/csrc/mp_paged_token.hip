@@ -22,7 +22,6 @@ typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
 constexpr int kWaves = 4, kTile = 32;
 constexpr int kPiece = kTile * 256, kSlot = 2 * kPiece, kRing = 2 * kSlot;
-constexpr int kWorkgroups = 256;
 // A part: weighted values as the lanes hold them, then maxima, then sums.
 constexpr int part_floats(int groups) { return 16 * groups * kHeadDim + 2 * 16 * groups; }
 constexpr size_t kCutFloats = sizeof(Cut) / sizeof(float) * kWorkgroups;
@@ -52,7 +51,7 @@ struct Source {
 };
 
 // Tiles [t0, t1) of 32 keys through one wave; `ring`: LDS offset of its ring.
-// kOnePage: pages of 32 rows or more, which hold whole tiles, so that a tile's address is a scalar.
+// kOnePage: pages of 16 rows or more, which hold halves of tiles, so that their addresses are scalars.
 template <int kGroups, bool kOnePage>
 __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, const bf16x8 (&q)[kGroups][4], int t0, int t1, uint32_t ring,
                                        const int (&position)[kGroups], int pos_min, int pos_max, int window, float scale)
@@ -64,25 +63,27 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
     const uint32_t v_at = ring + kPiece + (uint32_t)(vr * 256 + ((((col & 3) >> 1) ^ ((vr & 7) << 1)) << 4) + (col & 1) * 8);      // ^ 32 d
 
     // (entries are looked at two tiles after they were asked for: looked at at once, they made the wave wait for all loads before them)
-    auto entry_at = [&](int t) { return c.entries[min(t * kTile + (kOnePage ? 0 : lane & 31), c.end - 1) >> c.shift]; };      // of key 32 t (+ lane % 32)
+    auto entry_at = [&](int t) { return c.entries[min(t * kTile + (kOnePage ? lane & 16 : lane & 31), c.end - 1) >> c.shift]; };      // of key 32 t + lane % 32, or of its half
     auto held = [&](int t, int entry) {
         if constexpr (kOnePage) {
             const int n = c.end - t * kTile;
-            return (uint32_t)__builtin_amdgcn_readfirstlane(entry) < (uint32_t)c.n_pages ? n >= 32 ? ~0u : (1u << n) - 1u : 0u;
+            const uint32_t in = ((uint32_t)lane_value(entry, 0) < (uint32_t)c.n_pages ? 0xffffu : 0u) | ((uint32_t)lane_value(entry, 16) < (uint32_t)c.n_pages ? 0xffff0000u : 0u);
+            return n >= 32 ? in : in & ((1u << n) - 1u);
         } else {
             return (uint32_t)__ballot(t * kTile + (lane & 31) < c.end && (uint32_t)entry < (uint32_t)c.n_pages);
         }
     };
-    // What a lane loads, in bytes from a tile's first row: rows 4 i + g, i = 0 .. 3 (of keys; 4 .. 7 are 4096 on) or 0, 1 (of values; 2 and on are 2048 on).
+    // What a lane loads, in bytes: rows 4 i + g of a half tile, i = 0 .. 3 (keys) or 0, 1 (values; 2 and 3 are 2048 on).
     uint32_t k_from[4], v_from[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) k_from[i] = (uint32_t)((4 * i + g) * 256 + ((col ^ (4 * i + g)) << 4));
 #pragma unroll
     for (int i = 0; i < 2; ++i) v_from[i] = (uint32_t)((4 * i + g) * 256 + ((col ^ ((4 * i + g) << 1)) << 4));
-    long long off[kOnePage ? 1 : 8];
-    auto offsets = [&](int t, int entry, uint32_t valid) {    // bytes, of the tile or of rows 4 i + g; those that are not there: somewhere in page 0
+    long long off[kOnePage ? 2 : 8];
+    auto offsets = [&](int t, int entry, uint32_t valid) {    // bytes, of the tile's halves or of rows 4 i + g; those that are not there: somewhere in page 0
         if constexpr (kOnePage) {
-            off[0] = row_of(valid ? __builtin_amdgcn_readfirstlane(entry) : 0, c.h, c.n_kv, c.shift, t * kTile) * 256;
+            off[0] = row_of(valid & 0xffffu ? lane_value(entry, 0) : 0, c.h, c.n_kv, c.shift, t * kTile) * 256;
+            off[1] = row_of(valid >> 16 ? lane_value(entry, 16) : 0, c.h, c.n_kv, c.shift, t * kTile + 16) * 256;
         } else {
             const int mine = (valid >> (lane & 31) & 1) ? entry : 0;
 #pragma unroll
@@ -93,7 +94,7 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t to = ring + (uint32_t)((t & 1) * kSlot + i * 1024);
-            if constexpr (kOnePage) load_to_lds(c.K + off[0] + (i >= 4 ? 4096 : 0) + k_from[i & 3], to);
+            if constexpr (kOnePage) load_to_lds(c.K + off[i >> 2] + k_from[i & 3], to);
             else load_to_lds(c.K + off[i] + (k_from[i & 3] & 255u), to);
         }
     };
@@ -101,7 +102,7 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t to = ring + (uint32_t)((t & 1) * kSlot + kPiece + i * 1024);
-            if constexpr (kOnePage) load_to_lds(c.V + off[0] + (i >> 1) * 2048 + v_from[i & 1], to);
+            if constexpr (kOnePage) load_to_lds(c.V + off[i >> 2] + ((i >> 1) & 1) * 2048 + v_from[i & 1], to);
             else load_to_lds(c.V + off[i] + (v_from[i & 1] & 255u), to);
         }
     };
@@ -311,9 +312,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
         bf16x8 q[kGroups][4];
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) {
-            const int row = min(16 * r + col, tile_rows - 1), i = it.tile * tl.tokens + row / G;
+            const int row = min(16 * r + col, tile_rows - 1), in_tile = token_of_row(tl, row), i = it.tile * tl.tokens + in_tile;
             token[r] = it.rows.q0 + i;
-            head[r] = h * G + row % G;
+            head[r] = h * G + row - in_tile * G;
             position[r] = it.rows.base + i;
             const uint4* from = reinterpret_cast<const uint4*>(a.q + (long long)token[r] * a.q_stride + (long long)head[r] * kHeadDim);
 #pragma unroll
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
             }
         }
         __syncthreads();
-        float* part = parts + (2ll * share + slot_of(blocks_from(it, tl, line, h), share, line.share)) * part_floats(kGroups);
+        float* part = parts + (2ll * share + slot_of(blocks_from(it, line, h), share, line.share)) * part_floats(kGroups);
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) {
             float M = -INFINITY, L = 0.f, f[kWaves];
@@ -468,18 +469,10 @@ __global__ __launch_bounds__(256) void paged_token_merge_kernel(PagedAttention a
 template <int kGroups>
 hipError_t launch(const PagedAttention& a, float* room, hipStream_t s)
 {
-    Tiling tl;
-    tl.group = a.n_q_heads / a.c.n_kv;
-    tl.tokens = 16 * kGroups / tl.group;
-    tl.over = 0;
-    tl.most = 16 * kGroups;
-    tl.unit = kWaves * kTile;
-    tl.ahead = 2;
-    tl.least = 1 + tl.ahead;
-    tl.workgroups = kWorkgroups;
+    const Tiling tl = tiling(a.n_q_heads / a.c.n_kv, 16 * kGroups, 0, 16 * kGroups, kWaves * kTile, 2, 1);
     Cut* cuts = reinterpret_cast<Cut*>(room);
     float* parts = room + kCutFloats;
-    const auto kernel = a.c.page_shift >= 5 ? paged_token_kernel<kGroups, true> : paged_token_kernel<kGroups, false>;
+    const auto kernel = a.c.page_shift >= 4 ? paged_token_kernel<kGroups, true> : paged_token_kernel<kGroups, false>;
     hipLaunchKernelGGL(kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
