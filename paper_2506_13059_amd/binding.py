@@ -124,6 +124,9 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+_stream_of = torch._C._cuda_getCurrentRawStream
+
+
 def _check(status, ctx=None):
     if status != MP_OK:
         msg = lib().mp_last_error(ctx).decode()
@@ -184,28 +187,27 @@ def _reject(msg):
     raise MpError(MP_EINVAL, msg)
 
 
-def _on_device(t, name, dtype, dims=None):
-    """A tensor of a call on the current device: its type and number of dimensions are what the kernels take them to be."""
-    if t.dtype is not dtype or not t.is_cuda or t.device.index != torch.cuda.current_device() or (dims is not None and t.dim() != dims):
-        _reject(f"{name}: {dtype}{'' if dims is None else f' of {dims} dimensions'} on the current device expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+# (a call for a few tokens is over in 5 us on the device: the checks look at each tensor once and ask for the current device once a call)
+def _dense(t, name, dtype, shape, device):
+    """A contiguous tensor on the current device, of the type and shape that the kernels take it to have."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+        _reject(f"{name}: a contiguous tensor {tuple(shape)} of {dtype} on the current device expected, got {tuple(t.shape)} with strides {t.stride()} of {t.dtype} "
+                f"on {t.device}")
     return t
 
 
-def _dense(t, name, dtype, shape):
-    _on_device(t, name, dtype)
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        _reject(f"{name}: a contiguous tensor {tuple(shape)} expected, got {tuple(t.shape)} with strides {t.stride()}")
-    return t
-
-
-def _token_rows(t, name):
+def _token_rows(t, name, device):
     """(tokens, heads, token stride) of a bf16 tensor [tokens, heads, 128] whose tokens may be apart, as in the rows of a fused projection."""
-    _on_device(t, name, torch.bfloat16, 3)
-    n, h, d = t.shape
-    s0, s1, s2 = t.stride()
-    if d != 128 or s2 != 1 or (h > 1 and s1 != 128):
-        _reject(f"{name}: [tokens, heads, 128] with each token's rows behind one another expected, got {(n, h, d)} with strides {(s0, s1, s2)}")
-    return n, h, s0 if n > 1 else 0
+    if t.dtype is torch.bfloat16 and t.get_device() == device and t.dim() == 3:
+        n, h, d = t.shape
+        s0, s1, s2 = t.stride()
+        if d == 128 and s2 == 1 and (s1 == 128 or h <= 1):
+            return n, h, s0 if n > 1 else 0
+    _reject(f"{name}: bf16 [tokens, heads, 128] on the current device, each token's rows behind one another, expected, got {tuple(t.shape)} with strides {t.stride()} of "
+            f"{t.dtype} on {t.device}")
+
+
+_here = torch.cuda.current_device
 
 
 def mp_rotary_frequencies(rot_dim=128, base=10000.0, scaling=MP_ROTARY_PLAIN, factor=1.0, original_len=0.0, low=1.0, high=32.0):
@@ -222,40 +224,44 @@ class MpRotary:
                  amplitude=1.0, freqs=None):
         if freqs is None:
             freqs = mp_rotary_frequencies(rot_dim, base, scaling, factor, original_len, low, high).cuda()
-        self.freqs = _dense(freqs, "freqs", torch.float64, (rot_dim // 2,))
+        self.freqs = _dense(freqs, "freqs", torch.float64, (rot_dim // 2,), _here())
+        self.device = self.freqs.get_device()
         self.spec = MpRotarySpec(self.freqs.data_ptr(), rot_dim, layout, amplitude)
         self.at = C.addressof(self.spec)
 
-    def _at(self, device):
-        if self.freqs.device != device:
-            _reject(f"the frequencies lie on {self.freqs.device}, the tensors on {device}")
+    def _on(self, device):
+        if self.device != device:
+            _reject(f"the frequencies lie on device {self.device}, the tensors on device {device}")
         return self.at
 
     def mp_rotary(self, x, positions=None, out=None, lookup_position=None, out_lookup=None):
         """x bf16 [tokens, heads, 128] at positions int32 [tokens] -> out (like x, densely packed; `out` may be x).  With a lookup_position:
         (out, out_lookup), out_lookup turned to that one position; positions may then be None for the second alone."""
-        n, h, stride = _token_rows(x, "x")
-        to_stride = 0
+        device = _here()
+        n, h, stride = _token_rows(x, "x", device)
+        to_stride = to = look = at = 0
         if positions is not None:
-            _dense(positions, "positions", torch.int32, (n,))
+            at = _dense(positions, "positions", torch.int32, (n,), device).data_ptr()
             if out is None:
-                out = torch.empty(n, h, 128, dtype=torch.bfloat16, device=x.device)
+                out = x.new_empty((n, h, 128))
             else:
-                no, ho, to_stride = _token_rows(out, "out")
-                if (no, ho) != (n, h):
+                no, ho, to_stride = _token_rows(out, "out", device)
+                if no != n or ho != h:
                     _reject(f"out: [{n}, {h}, 128] expected, got {tuple(out.shape)}")
+            to = out.data_ptr()
         elif out is not None or lookup_position is None:
             _reject("positions are missing")
         if lookup_position is not None:
             if out_lookup is None:
-                out_lookup = torch.empty(n, h, 128, dtype=torch.bfloat16, device=x.device)
-            _dense(out_lookup, "out_lookup", torch.bfloat16, (n, h, 128))
+                out_lookup = x.new_empty((n, h, 128))
+            else:
+                _dense(out_lookup, "out_lookup", torch.bfloat16, (n, h, 128), device)
+            look = out_lookup.data_ptr()
         elif out_lookup is not None:
             _reject("out_lookup needs a lookup_position")
-        st = lib().mp_rotary(self._at(x.device), x.data_ptr(), stride, None if positions is None else positions.data_ptr(), n, h,
-                             None if out is None else out.data_ptr(), to_stride, None if out_lookup is None else out_lookup.data_ptr(),
-                             lookup_position or 0, _stream())
-        _check(st)
+        st = lib().mp_rotary(self._on(device), x.data_ptr(), stride, at, n, h, to, to_stride, look, lookup_position or 0, _stream_of(device))
+        if st:
+            _check(st)
         return out if lookup_position is None else (out, out_lookup)
 
 
@@ -268,81 +274,89 @@ class MpPagedKv:
     kv_len int32 [n_seqs], q_start int32 [n_seqs + 1].  The tensors are kept, not copied: change them in place between calls."""
 
     def __init__(self, k_pages, v_pages, page_table, kv_len, q_start):
-        _on_device(k_pages, "k_pages", torch.bfloat16, 4)
+        device = self.device = _here()
+        if k_pages.dim() != 4 or page_table.dim() != 2:
+            _reject(f"k_pages [n_pages, Hkv, page_size, 128] and page_table [n_seqs, pages] expected, got {tuple(k_pages.shape)} and {tuple(page_table.shape)}")
         n_pages, self.n_kv_heads, page_size, d = k_pages.shape
-        _dense(k_pages, "k_pages", torch.bfloat16, k_pages.shape)
-        _dense(v_pages, "v_pages", torch.bfloat16, k_pages.shape)
-        _on_device(page_table, "page_table", torch.int32, 2)
         self.n_seqs = page_table.shape[0]
-        _dense(page_table, "page_table", torch.int32, page_table.shape)
-        _dense(kv_len, "kv_len", torch.int32, (self.n_seqs,))
-        _dense(q_start, "q_start", torch.int32, (self.n_seqs + 1,))
+        _dense(k_pages, "k_pages", torch.bfloat16, k_pages.shape, device)
+        _dense(v_pages, "v_pages", torch.bfloat16, k_pages.shape, device)
+        _dense(page_table, "page_table", torch.int32, page_table.shape, device)
+        _dense(kv_len, "kv_len", torch.int32, (self.n_seqs,), device)
+        _dense(q_start, "q_start", torch.int32, (self.n_seqs + 1,), device)
         self.tensors = (k_pages, v_pages, page_table, kv_len, q_start)
-        self.device = k_pages.device
         self.args = MpPagedKvArgs(*(t.data_ptr() for t in self.tensors), n_pages, page_size, self.n_kv_heads, d, self.n_seqs, page_table.shape[1])
         self.at = C.addressof(self.args)
 
-    def _here(self):
-        if self.device.index != torch.cuda.current_device():
-            _reject(f"the cache lies on {self.device}, not on the current device")
+    def _current(self):
+        device = _here()
+        if self.device != device:
+            _reject(f"the cache lies on device {self.device}, not on the current device {device}")
+        return device
 
     def mp_paged_append(self, k, v, rotary=None, q=None, q_out=None):
         """k, v bf16 [tokens, Hkv, 128] join the cache; returns the turned queries q_out [tokens, Hq, 128], or None without q."""
-        self._here()
-        n, h, ks = _token_rows(k, "k")
-        nv, hv, vs = _token_rows(v, "v")
-        if h != self.n_kv_heads or (nv, hv) != (n, h):
+        device = self._current()
+        n, h, ks = _token_rows(k, "k", device)
+        nv, hv, vs = _token_rows(v, "v", device)
+        if h != self.n_kv_heads or hv != h or nv != n:
             _reject(f"k, v: [tokens, {self.n_kv_heads}, 128] expected, got {tuple(k.shape)} and {tuple(v.shape)}")
-        hq = qs = 0
+        hq = qs = from_ = to = 0
         if q is not None:
-            nq, hq, qs = _token_rows(q, "q")
+            nq, hq, qs = _token_rows(q, "q", device)
             if nq != n:
                 _reject(f"q: {n} tokens expected, got {nq}")
             if q_out is None:
-                q_out = torch.empty(n, hq, 128, dtype=torch.bfloat16, device=q.device)
-            _dense(q_out, "q_out", torch.bfloat16, (n, hq, 128))
+                q_out = q.new_empty((n, hq, 128))
+            else:
+                _dense(q_out, "q_out", torch.bfloat16, (n, hq, 128), device)
+            from_, to = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             _reject("q_out needs q")
-        st = lib().mp_paged_append(self.at, None if rotary is None else rotary._at(self.device), None if q is None else q.data_ptr(), qs, hq,
-                                   None if q_out is None else q_out.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, n, _stream())
-        _check(st)
+        st = lib().mp_paged_append(self.at, None if rotary is None else rotary._on(device), from_, qs, hq, to, k.data_ptr(), ks, v.data_ptr(), vs, n,
+                                   _stream_of(device))
+        if st:
+            _check(st)
         return q_out
 
     def mp_paged_attention(self, q, max_new=0, window=0, softmax_scale=0.0, out=None, lse=None, workspace=None):
         """q bf16 [tokens, Hq, 128] -> out bf16 [tokens, Hq, 128] (and lse fp32 [tokens, Hq]); max_new: as many new tokens a sequence at most."""
-        self._here()
-        n, hq, qs = _token_rows(q, "q")
+        device = self._current()
+        n, hq, qs = _token_rows(q, "q", device)
         if out is None:
-            out = torch.empty(n, hq, 128, dtype=torch.bfloat16, device=q.device)
-        _dense(out, "out", torch.bfloat16, (n, hq, 128))
+            out = q.new_empty((n, hq, 128))
+        else:
+            _dense(out, "out", torch.bfloat16, (n, hq, 128), device)
         if lse is not None:
-            _dense(lse, "lse", torch.float32, (n, hq))
+            _dense(lse, "lse", torch.float32, (n, hq), device)
         if workspace is None:
             workspace = torch.empty(mp_paged_workspace_bytes(n, hq, self.n_kv_heads, self.n_seqs, max_new), dtype=torch.uint8, device=q.device)
-        else:
-            _on_device(workspace, "workspace", workspace.dtype)
+        elif workspace.get_device() != device or not workspace.is_contiguous():
+            _reject(f"workspace: a contiguous tensor on the current device expected, got one on {workspace.device}")
         st = lib().mp_paged_attention(self.at, q.data_ptr(), qs, n, hq, max_new, window, softmax_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                      _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
-        _check(st)
+                                      workspace.data_ptr(), workspace.nbytes, _stream_of(device))
+        if st:
+            _check(st)
         return out
 
     def mp_paged_gather(self, n, first=0, rotary=None, lookup_position=None, k=None, v=None, k_lookup=None):
         """Keys and values [first, first + n) of every sequence: (k, v) bf16 [n_seqs, Hkv, n, 128], with a lookup_position (k, v, k_lookup)."""
-        self._here()
-        shape = (self.n_seqs, self.n_kv_heads, n, 128)
+        device = self._current()
         if n < 0:
             _reject(f"n = {n} < 0")
-        k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.device) if t is None else _dense(t, "k, v", torch.bfloat16, shape) for t in (k, v))
+        shape, pages = (self.n_seqs, self.n_kv_heads, n, 128), self.tensors[0]
+        k, v = (pages.new_empty(shape) if t is None else _dense(t, "k, v", torch.bfloat16, shape, device) for t in (k, v))
+        look = 0
         if lookup_position is not None:
             if rotary is None:
                 _reject("a lookup_position needs the rotary that the keys were stored with")
-            k_lookup = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if k_lookup is None else _dense(k_lookup, "k_lookup", torch.bfloat16, shape)
+            k_lookup = pages.new_empty(shape) if k_lookup is None else _dense(k_lookup, "k_lookup", torch.bfloat16, shape, device)
+            look = k_lookup.data_ptr()
         elif k_lookup is not None:
             _reject("k_lookup needs a lookup_position")
-        if n > 0:
-            st = lib().mp_paged_gather(self.at, None if rotary is None else rotary._at(self.device), first, n, lookup_position or 0, k.data_ptr(),
-                                       None if k_lookup is None else k_lookup.data_ptr(), v.data_ptr(), _stream())
-            _check(st)
+        if n > 0 and self.n_seqs > 0:
+            _check(lib().mp_paged_gather(self.at, None if rotary is None else rotary._on(device), first, n, lookup_position or 0, k.data_ptr(), look, v.data_ptr(),
+                                         _stream_of(device)))
         return (k, v) if lookup_position is None else (k, v, k_lookup)
 
 
