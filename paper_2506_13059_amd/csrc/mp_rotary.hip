@@ -121,8 +121,18 @@ __device__ __forceinline__ void fill_table(float2* table, const Rotation& rot, i
 }
 
 constexpr int kWaves = 4;
+constexpr int kDeep = 4;           // groups of four rows whose loads are on their way together
+
+// kOnce: the results are more than the caches hold by the time someone wants them, and go past them (non-temporal).
+template <bool kOnce>
+__device__ __forceinline__ void store16(uint4* p, const uint4& v)
+{
+    if constexpr (kOnce) store_once(p, v);
+    else *p = v;
+}
 
 // One wave: `rows` rows (a multiple of four) of one token.
+template <bool kOnce>
 __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(Rotation rot, const uint16_t* x, long long x_stride, const int32_t* positions,
                                                              uint16_t* out, long long out_stride, uint16_t* lookup, int lookup_position,
                                                              int n_tokens, int n_heads, int rows, int parts)
@@ -142,18 +152,27 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(Rotation rot, const
         fixed = load_turn(tables[wave][1], rot);
     }
     const int end = min(n_heads, (part + 1) * rows);
-    for (int h0 = part * rows; h0 < end; h0 += 4) {
-        const int h = min(h0 + (lane >> 4), end - 1);       // (rows past the end repeat the last one: all lanes take part in the exchange)
-        const uint4 v = reinterpret_cast<const uint4*>(x + t * x_stride + (long long)h * kHeadDim)[c];
-        float y[8];
-        partners(v, out ? own : fixed, rot, y);
-        const bool mine = h0 + (lane >> 4) < end;
-        if (out && mine) reinterpret_cast<uint4*>(out + t * out_stride + (long long)h * kHeadDim)[c] = turned(v, y, own);
-        if (lookup && mine) reinterpret_cast<uint4*>(lookup + ((long long)t * n_heads + h) * kHeadDim)[c] = turned(v, y, fixed);
+    for (int h0 = part * rows; h0 < end; h0 += 4 * kDeep) {
+        uint4 v[kDeep];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {                   // (rows past the end repeat the last one: all lanes take part in the exchange)
+            const int h = min(h0 + 4 * i + (lane >> 4), end - 1);
+            v[i] = reinterpret_cast<const uint4*>(x + t * x_stride + (long long)h * kHeadDim)[c];
+        }
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const int h = h0 + 4 * i + (lane >> 4);
+            if (h0 + 4 * i >= end) break;
+            float y[8];
+            partners(v[i], out ? own : fixed, rot, y);
+            if (out && h < end) store16<kOnce>(reinterpret_cast<uint4*>(out + t * out_stride + (long long)h * kHeadDim) + c, turned(v[i], y, own));
+            if (lookup && h < end) store16<kOnce>(reinterpret_cast<uint4*>(lookup + ((long long)t * n_heads + h) * kHeadDim) + c, turned(v[i], y, fixed));
+        }
     }
 }
 
 // One wave: `rows` rows of one token, which are its query heads, then its key heads, then its value heads.
+template <bool kOnce>
 __global__ __launch_bounds__(64 * kWaves) void paged_append_kernel(PagedKv cache, Rotation rot, const uint16_t* q, long long q_stride,
                                                                    uint16_t* q_out, const uint16_t* k, long long k_stride, const uint16_t* v,
                                                                    long long v_stride, int n_tokens, int n_q, int rows, int parts)
@@ -171,25 +190,34 @@ __global__ __launch_bounds__(64 * kWaves) void paged_append_kernel(PagedKv cache
     fill_table(tables[wave], rot, position);
     const Turn turn = load_turn(tables[wave], rot);
     const int total = n_q + 2 * cache.n_kv, end = min(total, (part + 1) * rows);
-    for (int r0 = part * rows; r0 < end; r0 += 4) {
-        const int r = min(r0 + (lane >> 4), end - 1);
-        const int kv = r - n_q, h = kv < cache.n_kv ? kv : kv - cache.n_kv;
-        const uint16_t* from = kv < 0 ? q + t * q_stride + (long long)r * kHeadDim
-                               : kv < cache.n_kv ? k + t * k_stride + (long long)h * kHeadDim : v + t * v_stride + (long long)h * kHeadDim;
-        uint16_t* to;
-        if (kv < 0) to = q_out + ((long long)t * n_q + r) * kHeadDim;
-        else to = (kv < cache.n_kv ? cache.K : cache.V) + row_of(stored ? page : 0, h, cache.n_kv, cache.page_shift, position) * kHeadDim;
-        uint4 x = reinterpret_cast<const uint4*>(from)[c];
-        float y[8];
-        partners(x, turn, rot, y);
-        if (kv < cache.n_kv) x = turned(x, y, turn);
-        if (r0 + (lane >> 4) < end && (kv < 0 || stored)) reinterpret_cast<uint4*>(to)[c] = x;
+    for (int r0 = part * rows; r0 < end; r0 += 4 * kDeep) {
+        uint4 x[kDeep];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const int r = min(r0 + 4 * i + (lane >> 4), end - 1), kv = r - n_q, h = kv < cache.n_kv ? kv : kv - cache.n_kv;
+            const uint16_t* from = kv < 0 ? q + t * q_stride + (long long)r * kHeadDim
+                                   : kv < cache.n_kv ? k + t * k_stride + (long long)h * kHeadDim : v + t * v_stride + (long long)h * kHeadDim;
+            x[i] = reinterpret_cast<const uint4*>(from)[c];
+        }
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const int r = r0 + 4 * i + (lane >> 4), kv = r - n_q, h = kv < cache.n_kv ? kv : kv - cache.n_kv;
+            if (r0 + 4 * i >= end) break;
+            float y[8];
+            partners(x[i], turn, rot, y);
+            if (kv < cache.n_kv) x[i] = turned(x[i], y, turn);
+            uint16_t* to;
+            if (kv < 0) to = q_out + ((long long)t * n_q + r) * kHeadDim;
+            else to = (kv < cache.n_kv ? cache.K : cache.V) + row_of(stored ? page : 0, h, cache.n_kv, cache.page_shift, position) * kHeadDim;
+            if (r < end && (kv < 0 || stored)) store16<kOnce>(reinterpret_cast<uint4*>(to) + c, x[i]);
+        }
     }
 }
 
 constexpr int kGatherTokens = 16;
 
 // One workgroup: 16 positions of a sequence, all heads.
+template <bool kOnce>
 __global__ __launch_bounds__(64 * kWaves) void paged_gather_kernel(PagedKv cache, Rotation rot, int first, int n, int lookup_position, uint16_t* k,
                                                                    uint16_t* k_lookup, uint16_t* v, int blocks_per_seq)
 {
@@ -211,23 +239,26 @@ __global__ __launch_bounds__(64 * kWaves) void paged_gather_kernel(PagedKv cache
     Turn turn{};
     if (k_lookup) turn = load_turn(tables[threadIdx.x >> 4], rot);
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (int h = 0; h < cache.n_kv; ++h) {
-        const long long from = row_of(page, h, cache.n_kv, cache.page_shift, position) * kHeadDim;
-        const long long to = (((long long)b * cache.n_kv + h) * n + i) * kHeadDim;
-        uint4 x = zero;
-        if (k || k_lookup) {
-            if (held) x = reinterpret_cast<const uint4*>(cache.K + from)[c];
-            if (k && i < n) reinterpret_cast<uint4*>(k + to)[c] = x;
+    for (int h0 = 0; h0 < cache.n_kv; h0 += 2) {
+        uint4 x[2], z[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const long long from = row_of(held ? page : 0, min(h0 + e, cache.n_kv - 1), cache.n_kv, cache.page_shift, position) * kHeadDim;
+            x[e] = z[e] = zero;
+            if (held && (k || k_lookup)) x[e] = reinterpret_cast<const uint4*>(cache.K + from)[c];
+            if (held && v) z[e] = reinterpret_cast<const uint4*>(cache.V + from)[c];
         }
-        if (k_lookup) {
-            float y[8];
-            partners(x, turn, rot, y);
-            if (i < n) reinterpret_cast<uint4*>(k_lookup + to)[c] = turned(x, y, turn);
-        }
-        if (v) {
-            uint4 z = zero;
-            if (held) z = reinterpret_cast<const uint4*>(cache.V + from)[c];
-            if (i < n) reinterpret_cast<uint4*>(v + to)[c] = z;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if (h0 + e >= cache.n_kv) break;
+            const long long to = (((long long)b * cache.n_kv + h0 + e) * n + i) * kHeadDim;
+            if (k && i < n) store16<kOnce>(reinterpret_cast<uint4*>(k + to) + c, x[e]);
+            if (k_lookup) {
+                float y[8];
+                partners(x[e], turn, rot, y);
+                if (i < n) store16<kOnce>(reinterpret_cast<uint4*>(k_lookup + to) + c, turned(x[e], y, turn));
+            }
+            if (v && i < n) store16<kOnce>(reinterpret_cast<uint4*>(v + to) + c, z[e]);
         }
     }
 }
@@ -241,6 +272,10 @@ int rows_of_a_wave(int n_tokens, int total)
     return rows;
 }
 
+// Results of more than 64 MiB go past the caches.  Us with and without, the same tensors again and again: five prompts' append (486 MB moved) 76 and 100, gather with lookup keys
+// (336 MB) 57 and 77, (2.7 GB) 499 and 519; a prompt's queries (84 MB written) 28.4 and 28.9.
+bool past_caches(long long rows) { return rows * 256 > 64ll << 20; }
+
 }  // namespace
 
 hipError_t launch_rotary(const Rotation& rot, const TokenRows& x, const int32_t* positions, int n_tokens, uint16_t* out, long long out_stride,
@@ -249,7 +284,8 @@ hipError_t launch_rotary(const Rotation& rot, const TokenRows& x, const int32_t*
     if (n_tokens <= 0) return hipSuccess;
     const int rows = rows_of_a_wave(n_tokens, x.n_heads), parts = (x.n_heads + rows - 1) / rows;
     const long long blocks = ((long long)n_tokens * parts + kWaves - 1) / kWaves;
-    hipLaunchKernelGGL(rotary_kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, rot, x.p, x.stride, positions, out, out_stride, out_lookup,
+    const auto kernel = past_caches((long long)n_tokens * x.n_heads * ((out != nullptr) + (out_lookup != nullptr))) ? rotary_kernel<true> : rotary_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, rot, x.p, x.stride, positions, out, out_stride, out_lookup,
                        lookup_position, n_tokens, x.n_heads, rows, parts);
     return hipGetLastError();
 }
@@ -261,7 +297,8 @@ hipError_t launch_paged_append(const PagedKv& c, const Rotation& rot, const Toke
     const int total = q.n_heads + 2 * c.n_kv;
     const int rows = rows_of_a_wave(n_tokens, total), parts = (total + rows - 1) / rows;
     const long long blocks = ((long long)n_tokens * parts + kWaves - 1) / kWaves;
-    hipLaunchKernelGGL(paged_append_kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, c, rot, q.p, q.stride, q_out, k.p, k.stride, v.p, v.stride,
+    const auto kernel = past_caches((long long)n_tokens * total) ? paged_append_kernel<true> : paged_append_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, c, rot, q.p, q.stride, q_out, k.p, k.stride, v.p, v.stride,
                        n_tokens, q.n_heads, rows, parts);
     return hipGetLastError();
 }
@@ -271,7 +308,8 @@ hipError_t launch_paged_gather(const PagedKv& c, const Rotation& rot, int first,
 {
     if (n <= 0 || c.n_seqs <= 0) return hipSuccess;
     const int per = (n + kGatherTokens - 1) / kGatherTokens;
-    hipLaunchKernelGGL(paged_gather_kernel, dim3((unsigned)((long long)per * c.n_seqs)), dim3(64 * kWaves), 0, s, c, rot, first, n, lookup_position, k,
+    const auto kernel = past_caches((long long)c.n_seqs * c.n_kv * n * ((k != nullptr) + (k_lookup != nullptr) + (v != nullptr))) ? paged_gather_kernel<true> : paged_gather_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)per * c.n_seqs)), dim3(64 * kWaves), 0, s, c, rot, first, n, lookup_position, k,
                        k_lookup, v, per);
     return hipGetLastError();
 }
