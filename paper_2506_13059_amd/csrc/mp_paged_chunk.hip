@@ -1,7 +1,7 @@
 // Attention of many new tokens over a paged cache, on the matrix cores, for gfx950.  (mp_paged_attn.hip says what is computed.)
 //
 // Eight waves of 32 query rows each work on one item (mp_paged_plan.h): 64 keys and values at a time go straight to LDS (global_load_lds, 16 bytes a lane), into
-// a ring of four blocks, up to three blocks ahead.  S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16, so a lane holds one query row in both (its column): its softmax
+// a ring of four blocks, two in use and two on their way.  S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_32x32x16_bf16, so a lane holds one query row in both (its column): its softmax
 // needs no more of other lanes than one exchange of maxima, and the rows of S^T that it holds are, converted to bf16, what the second product takes from it,
 // with the values' rows read (transposed by LDS) in the same order.
 #include "mp_paged_plan.h"
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
         if (end > 0) {
             // what the wave knows of the rows on their way, a block ahead and more
-            uint32_t bits1, bits2 = 0, bits3 = 0;
+            uint32_t bits1, bits2, bits3 = 0;
             int entry = entry_at(first);
             const int entry1 = entry_at(min(first + 1, last - 1)), entry2 = entry_at(min(first + 2, last - 1));
             workgroup_sync();                              // (the item before is done with LDS)
@@ -325,23 +325,20 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             bits2 = bits_of(block, entry1);
             load_all(rows_at(block, first + 1, entry1, bits2));
             block = min(first + 2, last - 1);
-            bits3 = bits_of(block, entry2);
-            load_all(rows_at(block, first + 2, entry2, bits3));
-            block = min(first + 3, last - 1);
-            entry = entry_at(block);
-            wait_vm<8>();
+            entry = entry2;
+            wait_vm<0>();
             arrived(first, bits1);
+            if (first + 1 < last) arrived(first + 1, bits2);
             workgroup_sync();
             for (int t = first; t < last; ++t) {
                 const uint32_t slot = (uint32_t)((t & (kRing - 1)) * kBlockBytes);
-                // Block t + 3 takes the place of block t - 1.  A wave's four loads are spread over its products: eight waves' loads take the memory path some
-                // 500 cycles, in which a wave that asks for more has to stand.
-                bits1 = bits2;
+                // Waves meet behind every second block (behind each: 4.34 ms for 2048 tokens at 128K, now 4.27); block t + 2 takes the place of one that all of them were done with then.
+                // A wave's four loads are spread over its products: eight waves' loads take the memory path some 500 cycles, in which a wave that asks for more has to stand.
                 bits2 = bits3;
                 // (Past the share's end the last block is loaded again: a branch for that would cut the products' code into pieces.)
                 bits3 = bits_of(block, entry);
-                const Rows coming = rows_at(block, t + 3, entry, bits3);
-                block = min(t + 4, last - 1);
+                const Rows coming = rows_at(block, t + 2, entry, bits3);
+                block = min(t + 3, last - 1);
                 entry = entry_at(block);
                 // (with this as the `else` of what follows, its state was copied at the end of both, and registers ran out)
                 const bool sees_some = active && t * kKeys <= pos_max;
@@ -359,9 +356,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 for (int i = 0; i < 16; ++i) {
                     if (i == 8) read_keys(k, k_at ^ 128u, slot);
                     s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i & 7], q[i >> 1], s[i & 1], 0, 0, 0);
-                    if ((i & 7) == 3) {
+                    if ((i & 3) == 1) {
                         __builtin_amdgcn_sched_barrier(0);
-                        load(coming, i >> 3);
+                        load(coming, i >> 2);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
@@ -417,7 +414,6 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     const auto w = __builtin_shufflevector(v[2 * (i & 7)], v[2 * (i & 7) + 1], 0, 1, 2, 3, 4, 5, 6, 7);
                     st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), p[i >> 2], st.o[i & 3], 0, 0, 0);
                     if (i < 12) probabilities((i >> 2) + 1, 2 * (i & 3));
-                    if ((i & 7) == 3) load(coming, 2 + (i >> 3));
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 // Values that are not finite have been taken out of an edge's block, lest they meet the zero of a row that does not see them: they are
@@ -441,9 +437,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     }
                 }
             }
-                wait_vm<8>();
-                if (t + 1 < last) arrived(t + 1, bits1);
-                workgroup_sync();
+                if ((t - first) & 1) {
+                    wait_vm<0>();
+                    if (t + 1 < last) arrived(t + 1, bits2);
+                    if (t + 2 < last) arrived(t + 2, bits3);
+                    workgroup_sync();
+                }
             }
             wait_vm<0>();
         }
