@@ -16,9 +16,9 @@ namespace {
 
 constexpr double kTurn = 0.15915494309189533577;      // 1 / (2 pi)
 
-__device__ __forceinline__ float2 cos_sin(int position, double freq, float amplitude)
+__device__ __forceinline__ float2 cos_sin(double position, double freq, float amplitude)
 {
-    double turns = (double)position * freq * kTurn;
+    double turns = position * freq * kTurn;
     turns -= __builtin_rint(turns);
     float s, c;
     sincospif(2.f * (float)turns, &s, &c);
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_gather_kernel(PagedKv cache
     if (k_lookup) {
         for (int e = threadIdx.x; e < kGatherTokens * 64; e += 64 * kWaves) {
             const int pair = e & 63;
-            if (pair < (rot.rot_dim >> 1)) tables[e >> 6][pair] = cos_sin(lookup_position - (first + i0 + (e >> 6)), rot.freqs[pair], 1.f);
+            if (pair < (rot.rot_dim >> 1)) tables[e >> 6][pair] = cos_sin((double)lookup_position - (double)(first + i0 + (e >> 6)), rot.freqs[pair], 1.f);
         }
         __syncthreads();
     }

@@ -152,6 +152,35 @@ def test_attention_of_chunks(new, lens, G, page, Hkv, window):
     _attend(Batch(new, lens, Hkv, page, pad_front=3, pad_back=1), G * Hkv, window)
 
 
+def test_many_sequences_of_several_tiles():
+    n = [1 + (7 * i) % 90 for i in range(150)]
+    _attend(Batch(n, [k + (31 * i) % 400 for i, k in enumerate(n)], 1, 16, pad_front=5, pad_back=9), 8)
+    # the line of blocks is long enough for the places in front of items
+    _attend(Batch([1000, 3, 600, 1], [9000, 4000, 600, 12000], 8, 64), 32)
+    _attend(Batch([1] * 40, [3000 + 411 * i for i in range(40)], 8, 16), 16)
+
+
+def _random_batch(seed):
+    r = torch.Generator().manual_seed(seed)
+    pick = lambda *x: x[int(torch.randint(0, len(x), (1,), generator=r))]      # noqa: E731
+    size = lambda hi: int(math.exp(float(torch.rand(1, generator=r)) * math.log(hi)))      # noqa: E731
+    seqs, most = pick(1, 2, 3, 9, 33), pick(1, 1, 4, 12, 200, 600)
+    new = [min(most, size(most + 1)) if pick(0, 1, 1, 1) else 0 for _ in range(seqs)]
+    new[0] = max(new[0], 1)
+    lens = [max(0, k + size(4000) - pick(1, 1, 1, 4)) for k in new]
+    return dict(new=new, lens=lens, Hkv=pick(1, 2, 3), page=pick(4, 8, 16, 32, 64, 512), G=pick(1, 2, 3, 4, 5, 6, 7, 8), window=pick(0, 0, 1, 64, 333))
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_batches(seed):
+    c = _random_batch(seed)
+    print("case", {**c, "new": c["new"][:6], "lens": c["lens"][:6]}, flush=True)
+    b = Batch(c["new"], c["lens"], c["Hkv"], c["page"], seed=seed, pad_front=seed % 3, pad_back=seed % 2)
+    if seed % 3 == 0:
+        b.table[(torch.rand(b.table.shape, generator=torch.Generator().manual_seed(seed)) < 0.1).cuda()] = -1
+    _attend(b, c["Hkv"] * c["G"], c["window"])
+
+
 @pytest.mark.parametrize("new,lens", [([1, 1], [3000, 2000]), ([70, 1], [400, 2000]), ([260], [4000])])
 def test_missing_pages_take_no_part(new, lens):
     b = Batch(new, lens, 2, 16)
@@ -256,6 +285,30 @@ def test_shared_pages():
     q[1] = q[0]
     out = b.paged().mp_paged_attention(q, max_new=1)
     assert torch.equal(out[0], out[1])
+
+
+def test_caches_of_more_than_32_bits():
+    # 5.4 GB of keys and as many of values: the sequence's pages are the last ones, and the first
+    mp = _mp()
+    n_pages, Hkv, page, n = 41000, 8, 64, 300
+    K, V = (torch.empty(n_pages, Hkv, page, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert K.numel() * 2 > 1 << 32
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 2, 32768, n_pages - 3]], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    big = mp.MpPagedKv(K, V, table, torch.tensor([n], dtype=torch.int32, device="cuda"), starts)
+    b = Batch([n], [n], Hkv, page)
+    k, v = b.keys[0].transpose(0, 1).contiguous(), b.values[0].transpose(0, 1).contiguous()
+    big.mp_paged_append(k, v)
+    gk, gv = big.mp_paged_gather(n)
+    assert torch.equal(gk[0], b.keys[0]) and torch.equal(gv[0], b.values[0])
+    q = _rows(n, 16, 3, 2.0)
+    assert torch.equal(big.mp_paged_attention(q), b.paged().mp_paged_attention(q))
+    one = mp.MpPagedKv(K, V, table, torch.tensor([n], dtype=torch.int32, device="cuda"), torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
+    out = one.mp_paged_attention(q[-1:], max_new=1)
+    b1 = Batch([1], [n], Hkv, page)
+    b1.keys, b1.values = b.keys, b.values
+    b1.write()
+    assert torch.equal(out, b1.paged().mp_paged_attention(q[-1:], max_new=1))
 
 
 def test_refusals():

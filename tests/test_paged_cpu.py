@@ -58,9 +58,21 @@ def where(tmp_path_factory):
 extern "C" int page(const int* row, int stride, int n_pages, int shift, int position) {{ return mp::page_of(row, stride, n_pages, shift, position); }}
 extern "C" long long row(int page, int head, int n_kv, int shift, int position) {{ return mp::row_of(page, head, n_kv, shift, position); }}
 ''')
+    src.write_text(src.read_text() + '''
+extern "C" void blocks(int base, int i0, int i1, int window, int room, int unit, int* out) { mp::blocks_of(base, i0, i1, window, room, unit, out, out + 1); }
+extern "C" void parts(long long x0, long long x1, long long share, long long* out)
+{
+    const mp::Parts p = mp::parts_of(x0, x1, share);
+    out[0] = p.first;
+    out[1] = p.last;
+}
+extern "C" int slot(long long x0, long long workgroup, long long share) { return mp::slot_of(x0, workgroup, share); }
+''')
     subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", "-o", str(so), str(src)])
     h = C.CDLL(str(so))
     h.row.restype = C.c_longlong
+    h.parts.argtypes = [C.c_longlong] * 3 + [C.POINTER(C.c_longlong)]
+    h.slot.argtypes = [C.c_longlong] * 3
     return h
 
 
@@ -74,6 +86,45 @@ def test_pages_that_are_not_there(where):
 def test_rows_pass_32_bits(where):
     assert where.row(3, 1, 2, 4, 37) == (3 * 2 + 1) * 16 + 5
     assert where.row(2 ** 31 - 1, 7, 8, 10, 2 ** 31 - 1) == (((2 ** 31 - 1) * 8 + 7) << 10) + 1023
+
+
+def test_blocks_are_those_of_the_keys_that_are_attended(where):
+    rng = np.random.default_rng(3)
+    out = (C.c_int * 2)()
+    for _ in range(3000):
+        unit, n = int(rng.choice([64, 128])), int(rng.integers(1, 60))
+        length, window = int(rng.integers(0, 900)), int(rng.choice([0, 0, 1, 37, 300]))
+        base, room = length - n, int(rng.choice([1 << 20, 300, 64]))
+        i0 = int(rng.integers(0, n))
+        i1 = int(rng.integers(i0, n))
+        keys = [j for i in (i0, i1) for j in range(max(0, base + i - window + 1) if window else 0, min(base + i + 1, room))]
+        where.blocks(base, i0, i1, window, room, unit, out)
+        assert out[1] > out[0] >= 0
+        if keys:
+            assert out[0] * unit <= min(keys) and max(keys) < out[1] * unit
+            assert min(keys) < (out[0] + 1) * unit and max(keys) >= (out[1] - 1) * unit      # (and no more)
+    where.blocks(2 ** 31 - 1 - 8, 0, 7, 0, 2 ** 31 - 1, 64, out)
+    assert list(out) == [0, 2 ** 25]
+
+
+def test_parts_of_items_have_places_of_their_own(where):
+    # items one after another on a line that is cut into shares: every block of an item lies in one of its parts, and no two parts of different items share a slot
+    rng = np.random.default_rng(4)
+    out = (C.c_longlong * 2)()
+    for _ in range(300):
+        share, ahead, x, used = int(rng.integers(1, 40)), int(rng.integers(0, 4)), 0, {}
+        for item in range(40):
+            x0 = x + ahead
+            x = x1 = x0 + int(rng.integers(1, 90))
+            where.parts(x0, x1, share, out)
+            first, last = out[0], out[1]
+            assert first * share <= x0 < (first + 1) * share and last * share < x1 <= (last + 1) * share
+            if first == last:
+                continue
+            for g in range(first, last + 1):
+                at = g, where.slot(x0, g, share)
+                assert at[1] == (0 if g > first else int(x0 > g * share)) and at not in used
+                used[at] = item
 
 
 # (addresses that no one reads: every call is refused before a launch)
