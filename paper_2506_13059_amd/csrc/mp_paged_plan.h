@@ -68,6 +68,23 @@ __device__ __forceinline__ void blocks_of_tile(const PagedAttention& a, const Ti
 }
 
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ int tiles_of(const Tiling& tl, const SequenceRows& r)
+{
+    const long long rows = (long long)r.n * tl.group;
+    return rows > tl.over && rows <= tl.most ? (r.n + tl.tokens - 1) / tl.tokens : 0;
+}
+// The item of lane `at`, whose places end at incl.
+__device__ __forceinline__ void take_item(Item* it, int at, int b, int tile, const SequenceRows& r, int b0, int b1, uint32_t incl, int ahead)
+{
+    it->b = lane_value(b, at);
+    it->tile = lane_value(tile, at);
+    it->rows.q0 = lane_value(r.q0, at);
+    it->rows.n = lane_value(r.n, at);
+    it->rows.base = lane_value(r.base, at);
+    it->b0 = lane_value(b0, at);
+    it->b1 = lane_value(b1, at);
+    it->before = (uint32_t)lane_value((int)incl, at) - (uint32_t)(ahead + it->b1 - it->b0);
+}
 
 // Places of one head's items in all, `ahead` of them in front of each one's blocks (*items: how many there are); kFind: up to the item that place x of the line
 // lies in, which goes to *found.  One wave, 64 sequences (or, where some have several tiles, 64 tiles) at a time.  `head`: rows_of_lane(a, 0).
@@ -78,8 +95,7 @@ __device__ __forceinline__ uint32_t walk(const PagedAttention& a, const Tiling& 
     uint32_t sum = 0;
     for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
         const SequenceRows r = s0 == 0 ? head : rows_of_lane(a, s0);
-        const long long rows = (long long)r.n * tl.group;
-        const int tiles = rows > tl.over && rows <= tl.most ? (r.n + tl.tokens - 1) / tl.tokens : 0;
+        const int tiles = tiles_of(tl, r);
         const bool several = __any(tiles > 1);
         const int upto = several ? (int)wave_incl_scan_u32((uint32_t)tiles) : 0;
         const int all = several ? lane_value(upto, 63) : 64;
@@ -105,15 +121,7 @@ __device__ __forceinline__ uint32_t walk(const PagedAttention& a, const Tiling& 
             if constexpr (kFind) {
                 const unsigned long long past = __ballot(sum + incl > x);
                 if (past) {
-                    const int at = __ffsll((long long)past) - 1;
-                    found->b = s0 + lane_value(k, at);
-                    found->tile = lane_value(tile, at);
-                    found->rows.q0 = lane_value(m.q0, at);
-                    found->rows.n = lane_value(m.n, at);
-                    found->rows.base = lane_value(m.base, at);
-                    found->b0 = lane_value(b0, at);
-                    found->b1 = lane_value(b1, at);
-                    found->before = sum + (uint32_t)lane_value((int)incl, at) - (uint32_t)(ahead + found->b1 - found->b0);
+                    take_item(found, __ffsll((long long)past) - 1, s0 + k, tile, m, b0, b1, sum + incl, ahead);
                     return sum;
                 }
             }
@@ -130,6 +138,10 @@ struct Line {
     int ahead;
     long long all, share;
     int used;                 // workgroups with a share
+    // up to 64 sequences of one tile or none (a decode step) are one look: the lane's blocks, and where its places end
+    bool one_look;
+    int b0, b1;
+    uint32_t incl;
 };
 // x / d (a line of 2^32 places or more is possible in principle only)
 __device__ __forceinline__ long long quotient(long long x, long long d)
@@ -141,10 +153,22 @@ __device__ __forceinline__ Line line_of(const PagedAttention& a, const Tiling& t
     Line l;
     l.head = rows_of_lane(a, 0);
     uint32_t items = 0;
-    l.of_head = walk<false>(a, tl, l.head, 0, 0, nullptr, &items);
+    const int tiles = tiles_of(tl, l.head);
+    const unsigned long long there = __ballot(tiles > 0);
+    l.one_look = a.c.n_seqs <= 64 && !__any(tiles > 1);
+    if (l.one_look) {
+        l.b0 = l.b1 = 0;
+        if (tiles > 0) blocks_of_tile(a, tl, l.head, 0, &l.b0, &l.b1);
+        l.incl = wave_incl_scan_u32((uint32_t)(l.b1 - l.b0));
+        l.of_head = (uint32_t)lane_value((int)l.incl, 63);
+        items = (uint32_t)__popcll(there);
+    } else {
+        l.of_head = walk<false>(a, tl, l.head, 0, 0, nullptr, &items);
+    }
     // (where shares are a few blocks anyway, every workgroup is worth more than evenness)
     l.ahead = (long long)l.of_head * a.c.n_kv >= 8 * kWorkgroups ? tl.ahead : 0;
     l.of_head += (uint32_t)l.ahead * items;
+    if (l.one_look) l.incl += (uint32_t)l.ahead * (uint32_t)__popcll(there & (~0ull >> (63 - (threadIdx.x & 63))));
     l.all = (long long)l.of_head * a.c.n_kv;
     l.share = max((l.all + kWorkgroups - 1) / kWorkgroups, (long long)(tl.least + l.ahead));
     l.used = (int)quotient(l.all + l.share - 1, l.share);
@@ -177,7 +201,9 @@ __device__ __forceinline__ void segment_at(const PagedAttention& a, const Tiling
         blocks_of_tile(a, tl, it.rows, ++it.tile, &it.b0, &it.b1);
     } else {
         s->h = (int)quotient(x, line.of_head);
-        walk<true>(a, tl, line.head, line.ahead, (uint32_t)(x - (long long)s->h * line.of_head), &it, nullptr);
+        const uint32_t of_this = (uint32_t)(x - (long long)s->h * line.of_head);
+        if (line.one_look) take_item(&it, __ffsll((long long)__ballot(line.incl > of_this)) - 1, threadIdx.x & 63, 0, line.head, line.b0, line.b1, line.incl, line.ahead);
+        else walk<true>(a, tl, line.head, line.ahead, of_this, &it, nullptr);
     }
     const long long x0 = blocks_from(it, line, s->h), x1 = x0 + (it.b1 - it.b0);
     s->next = min(x1, end);
