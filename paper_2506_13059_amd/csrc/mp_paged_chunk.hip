@@ -163,7 +163,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     __shared__ __align__(256) unsigned char lds[kRing * kBlockBytes + 2 * kRing * kWaves];
     const uint32_t ring = lds_offset(lds), valid_at = ring + kRing * kBlockBytes, odd_at = valid_at + kRing * kWaves;      // (a byte a wave: keys that are there; whose values are not all finite)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-    const Line line = line_of(a, tl);
+    Line line = line_of<false>(a, tl);
     const int share = share_of(line, blockIdx.x);
     if (share >= line.used) {
         if (threadIdx.x == 0) cuts[share].parts = 0;
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     Cut cut{};
     Segment seg;
     for (bool known = false; x < x_end; known = true, x = seg.next) {
-        segment_at(a, tl, line, x, x_end, known, &seg);
+        segment_at<false>(a, tl, line, x, x_end, known, &seg);
         const Item& it = seg.it;
         const int h = seg.h, first = seg.first, last = seg.last;
         if (first == last) continue;                       // (the share ends among the places in front)
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const float l = over_halves_sum(st.l);
         if (whole) store_rows(a, st, l, it.rows.q0 + i, head, wave * 32 + (lane & 31) < tile_rows);
         else {
-            store_part(parts + (2ll * share + slot_of(blocks_from(it, line, h), share, line.share)) * kPartFloats, st, l);
+            if (active) store_part(parts + (2ll * share + slot_of(blocks_from(it, line, h), share, line.share)) * kPartFloats, st, l);
             if (last < it.b1) cut = cut_of(it, tl, line, share, h);
         }
     }

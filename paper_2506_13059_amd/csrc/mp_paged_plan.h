@@ -86,8 +86,8 @@ __device__ __forceinline__ void take_item(Item* it, int at, int b, int tile, con
     it->before = (uint32_t)lane_value((int)incl, at) - (uint32_t)(ahead + it->b1 - it->b0);
 }
 
-// Places of one head's items in all, `ahead` of them in front of each one's blocks (*items: how many there are); kFind: up to the item that place x of the line
-// lies in, which goes to *found.  One wave, 64 sequences (or, where some have several tiles, 64 tiles) at a time.  `head`: rows_of_lane(a, 0).
+// Returns the places of one head's items in all, `ahead` of them in front of each one's blocks (*items: how many there are); kFind: goes up to the item that
+// place x of the line lies in, puts it into *found and returns x (anything else: there is none).  One wave, 64 sequences (or, where some have several tiles, 64 tiles) at a time.  `head`: rows_of_lane(a, 0).
 template <bool kFind>
 __device__ __forceinline__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const SequenceRows& head, int ahead, uint32_t x, Item* found, uint32_t* items)
 {
@@ -122,13 +122,13 @@ __device__ __forceinline__ uint32_t walk(const PagedAttention& a, const Tiling& 
                 const unsigned long long past = __ballot(sum + incl > x);
                 if (past) {
                     take_item(found, __ffsll((long long)past) - 1, s0 + k, tile, m, b0, b1, sum + incl, ahead);
-                    return sum;
+                    return x;
                 }
             }
             sum += (uint32_t)lane_value((int)incl, 63);
         }
     }
-    return sum;
+    return kFind ? x + 1 : sum;
 }
 
 // The line and its shares.  Neighbouring shares go to workgroups of one XCD: they mostly work on one head, whose keys its L2 then holds once.
@@ -138,37 +138,57 @@ struct Line {
     int ahead;
     long long all, share;
     int used;                 // workgroups with a share
-    // up to 64 sequences of one tile or none (a decode step) are one look: the lane's blocks, and where its places end
-    bool one_look;
-    int b0, b1;
-    uint32_t incl;
+    // The 64 sequences looked at, if none has more than one tile: the lane's blocks, and where its places end in the `total` of them behind the `before` of those
+    // before s0.
+    bool look;
+    int s0, b0, b1;
+    uint32_t before, total, incl;
 };
 // x / d (a line of 2^32 places or more is possible in principle only)
 __device__ __forceinline__ long long quotient(long long x, long long d)
 {
     return ((x | d) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;
 }
+// Looks at sequences s0 .., whose rows are in l->head.
+__device__ __forceinline__ void look_at(const PagedAttention& a, const Tiling& tl, Line* l, int s0, uint32_t before)
+{
+    const bool there = tiles_of(tl, l->head) > 0;
+    l->s0 = s0;
+    l->before = before;
+    l->b0 = l->b1 = 0;
+    if (there) blocks_of_tile(a, tl, l->head, 0, &l->b0, &l->b1);
+    l->incl = wave_incl_scan_u32(there ? (uint32_t)(l->ahead + l->b1 - l->b0) : 0u);
+    l->total = (uint32_t)lane_value((int)l->incl, 63);
+}
+// kSingle: no sequence of the tiling has more than one tile.
+template <bool kSingle>
 __device__ __forceinline__ Line line_of(const PagedAttention& a, const Tiling& tl)
 {
     Line l;
     l.head = rows_of_lane(a, 0);
+    l.ahead = 0;
+    l.look = kSingle || (a.c.n_seqs <= 64 && !__any(tiles_of(tl, l.head) > 1));
     uint32_t items = 0;
-    const int tiles = tiles_of(tl, l.head);
-    const unsigned long long there = __ballot(tiles > 0);
-    l.one_look = a.c.n_seqs <= 64 && !__any(tiles > 1);
-    if (l.one_look) {
-        l.b0 = l.b1 = 0;
-        if (tiles > 0) blocks_of_tile(a, tl, l.head, 0, &l.b0, &l.b1);
-        l.incl = wave_incl_scan_u32((uint32_t)(l.b1 - l.b0));
-        l.of_head = (uint32_t)lane_value((int)l.incl, 63);
-        items = (uint32_t)__popcll(there);
+    if (l.look) {
+        l.of_head = 0;
+        for (int s0 = 0;;) {
+            look_at(a, tl, &l, s0, l.of_head);
+            l.of_head += l.total;
+            items += (uint32_t)__popcll(__ballot(l.b1 > l.b0));
+            s0 += 64;
+            if (s0 >= a.c.n_seqs) break;
+            l.head = rows_of_lane(a, s0);
+        }
     } else {
         l.of_head = walk<false>(a, tl, l.head, 0, 0, nullptr, &items);
     }
     // (where shares are a few blocks anyway, every workgroup is worth more than evenness)
     l.ahead = (long long)l.of_head * a.c.n_kv >= 8 * kWorkgroups ? tl.ahead : 0;
     l.of_head += (uint32_t)l.ahead * items;
-    if (l.one_look) l.incl += (uint32_t)l.ahead * (uint32_t)__popcll(there & (~0ull >> (63 - (threadIdx.x & 63))));
+    if (l.look && (l.ahead || l.s0)) {
+        if (l.s0) l.head = rows_of_lane(a, 0);
+        look_at(a, tl, &l, 0, 0);
+    }
     l.all = (long long)l.of_head * a.c.n_kv;
     l.share = max((l.all + kWorkgroups - 1) / kWorkgroups, (long long)(tl.least + l.ahead));
     l.used = (int)quotient(l.all + l.share - 1, l.share);
@@ -193,17 +213,39 @@ __device__ __forceinline__ long long blocks_from(const Item& it, const Line& lin
     return (long long)h * line.of_head + it.before + line.ahead;
 }
 // `known`: s->it is the item before, which ended at x.
-__device__ __forceinline__ void segment_at(const PagedAttention& a, const Tiling& tl, const Line& line, long long x, long long end, bool known, Segment* s)
+template <bool kSingle>
+__device__ __forceinline__ void segment_at(const PagedAttention& a, const Tiling& tl, Line& line, long long x, long long end, bool known, Segment* s)
 {
     Item& it = s->it;
-    if (known && (it.tile + 1) * tl.tokens < it.rows.n) {
+    bool found = true;
+    if (!kSingle && known && (it.tile + 1) * tl.tokens < it.rows.n) {
         it.before += (uint32_t)(line.ahead + it.b1 - it.b0);
         blocks_of_tile(a, tl, it.rows, ++it.tile, &it.b0, &it.b1);
     } else {
         s->h = (int)quotient(x, line.of_head);
         const uint32_t of_this = (uint32_t)(x - (long long)s->h * line.of_head);
-        if (line.one_look) take_item(&it, __ffsll((long long)__ballot(line.incl > of_this)) - 1, threadIdx.x & 63, 0, line.head, line.b0, line.b1, line.incl, line.ahead);
-        else walk<true>(a, tl, line.head, line.ahead, of_this, &it, nullptr);
+        if (line.look) {
+            if constexpr (kSingle) {         // (from the sequences looked at last, or from the first)
+                while (of_this < line.before || of_this - line.before >= line.total) {
+                    const bool again = of_this < line.before;
+                    const int s0 = again ? 0 : line.s0 + 64;
+                    const uint32_t before = again ? 0 : line.before + line.total;
+                    if (s0 >= a.c.n_seqs) break;
+                    line.head = rows_of_lane(a, s0);
+                    look_at(a, tl, &line, s0, before);
+                }
+            }
+            found = of_this - line.before < line.total;
+            const int at = found ? __ffsll((long long)__ballot(line.incl > of_this - line.before)) - 1 : 0;
+            take_item(&it, at, line.s0 + (threadIdx.x & 63), 0, line.head, line.b0, line.b1, line.before + line.incl, line.ahead);
+        } else {
+            found = walk<true>(a, tl, line.head, line.ahead, of_this, &it, nullptr) == of_this;
+        }
+    }
+    if (!found) {                            // (lengths that change under the launch: nothing is done for them, but it ends)
+        s->first = s->last = 0;
+        s->next = end;
+        return;
     }
     const long long x0 = blocks_from(it, line, s->h), x1 = x0 + (it.b1 - it.b0);
     s->next = min(x1, end);

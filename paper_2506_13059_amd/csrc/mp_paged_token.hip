@@ -288,7 +288,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
     constexpr int kRows = 16 * kGroups;
     __shared__ __align__(256) unsigned char lds[kWaves * kRing + 2 * kWaves * kRows * 4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
-    const Line line = line_of(a, tl);
+    Line line = line_of<true>(a, tl);
     const int share = share_of(line, blockIdx.x);
     if (share >= line.used) {
         if (threadIdx.x == 0) cuts[share].parts = 0;
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
     Cut cut{};
     Segment seg;
     for (bool known = false; x < x_end; known = true, x = seg.next) {
-        segment_at(a, tl, line, x, x_end, known, &seg);
+        segment_at<true>(a, tl, line, x, x_end, known, &seg);
         const Item& it = seg.it;
         const int h = seg.h, first = seg.first, last = seg.last;
         if (first == last) continue;                       // (the share ends among the places in front)
