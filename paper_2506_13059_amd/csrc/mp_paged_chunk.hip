@@ -163,6 +163,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     __shared__ __align__(256) unsigned char lds[kRing * kBlockBytes + 2 * kRing * kWaves];
     const uint32_t ring = lds_offset(lds), valid_at = ring + kRing * kBlockBytes, odd_at = valid_at + kRing * kWaves;      // (a byte a wave: keys that are there; whose values are not all finite)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+    const float top = hidden_infinity();
     Line line = line_of<false>(a, tl);
     const int share = share_of(line, blockIdx.x);
     if (share >= line.used) {
@@ -380,9 +381,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 }
                 float part[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) part[j] = fmaxf(s[0][j], s[1][j]);
+                for (int j = 0; j < 4; ++j) part[j] = larger(s[0][j], s[1][j], top);
 #pragma unroll
-                for (int j = 4; j < 16; ++j) part[j & 3] = fmaxf(part[j & 3], fmaxf(s[0][j], s[1][j]));
+                for (int j = 4; j < 16; ++j) part[j & 3] = fmaxf(part[j & 3], larger(s[0][j], s[1][j], top));
                 float mx = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
                 mx = over_halves_max(mx) * scale;
                 // The maximum in use may be up to 2^8 behind: sums in fp32 and products of bf16 have room for it, and it is soon never moved.

@@ -14,6 +14,16 @@ namespace mp {
 
 namespace {
 
+// The larger of two numbers, `top` being infinity as a value that the compiler does not know.  (Of products of the matrix cores, fmaxf first takes each through an
+// instruction of its own, lest it be a signalling NaN.)
+__device__ __forceinline__ float larger(float a, float b, float top) { return __builtin_amdgcn_fmed3f(a, b, top); }
+__device__ __forceinline__ float hidden_infinity()
+{
+    float top = INFINITY;
+    asm volatile("" : "+s"(top));
+    return top;
+}
+
 // A sequence is an item's if it has more than `over` and at most `most` rows.
 struct Tiling {
     int group;                // G

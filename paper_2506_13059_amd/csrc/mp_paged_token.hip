@@ -56,6 +56,7 @@ template <int kGroups, bool kOnePage>
 __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, const bf16x8 (&q)[kGroups][4], int t0, int t1, uint32_t ring,
                                        const int (&position)[kGroups], int pos_min, int pos_max, int window, float scale)
 {
+    const float top = hidden_infinity();
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     // LDS: chunk j (16 bytes) of key r lies at j ^ r % 16, of value r at j ^ 2 (r % 8): the lanes of a read touch different banks
     const uint32_t k_at = ring + (uint32_t)(col * 256 + ((g ^ col) << 4));                                  // ^ 64 ks
@@ -170,7 +171,10 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
         bool grown = false;
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) {
-            mx[r] = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])), fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3]))) * scale;
+            mx[r] = larger(s[r][0][0], s[r][1][0], top);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) mx[r] = fmaxf(mx[r], larger(s[r][0][i], s[r][1][i], top));
+            mx[r] *= scale;
             grown |= mx[r] > st.m[r] + 8.f;
         }
         // The maximum in use may be up to 2^8 behind: sums in fp32 and products of bf16 have room for it, and it is soon never moved.
