@@ -16,6 +16,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
@@ -193,15 +194,30 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
                     for (int i = 0; i < 4; ++i) st.o[r][d][i] *= f;
             }
         }
-        bf16x8 p[kGroups];
+        // Probabilities are two bf16 values each where the products for that cost nothing (up to 32 rows): what truncation leaves of one is the second, an error of 2^-17.
+        // Four groups take them rounded to bf16 (2^-9).
+        constexpr bool kTwo = kGroups <= 2;
+        bf16x8 p[kGroups], p2[kTwo ? kGroups : 1];
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) {
             const float m = st.m[r] == -INFINITY ? 0.f : st.m[r];
+            float e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[r][i >> 2][i & 3], scale, -m));
-                st.l[r] += e;
-                p[r][i] = (__bf16)e;
+                e[i] = __builtin_amdgcn_exp2f(fmaf(s[r][i >> 2][i & 3], scale, -m));
+                st.l[r] += e[i];
+                if constexpr (!kTwo) p[r][i] = (__bf16)e[i];
+                else p2[r][i] = (__bf16)(e[i] - __uint_as_float(__float_as_uint(e[i]) & 0xffff0000u));
+            }
+            if constexpr (kTwo) {
+                u32x4 top_halves;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top_halves[i] = __builtin_amdgcn_perm(__float_as_uint(e[2 * i + 1]), __float_as_uint(e[2 * i]), 0x07060302u);
+                p[r] = __builtin_bit_cast(bf16x8, top_halves);
+                // (a second part of zero would make an infinite value NaN: it is 2^-126 at least, or the probability if that is less)
+                const u16x8 tiny = {0x0080, 0x0080, 0x0080, 0x0080, 0x0080, 0x0080, 0x0080, 0x0080};
+                const u16x8 floor = __builtin_elementwise_min(__builtin_bit_cast(u16x8, top_halves), tiny);
+                p2[r] = __builtin_bit_cast(bf16x8, __builtin_elementwise_max(__builtin_bit_cast(u16x8, p2[r]), floor));
             }
         }
         wait_vm<kAhead == 2 ? 24 : 16 * kAhead>();
@@ -245,8 +261,11 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
             for (int d = 0; d < 4; ++d) {
                 const auto a = __builtin_shufflevector(v[2 * d], v[2 * d + 1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int r = 0; r < kGroups; ++r)
+                for (int r = 0; r < kGroups; ++r) {
                     st.o[r][4 * d4 + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), p[r], st.o[r][4 * d4 + d], 0, 0, 0);
+                    if constexpr (kTwo)
+                        st.o[r][4 * d4 + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), p2[r], st.o[r][4 * d4 + d], 0, 0, 0);
+                }
             }
         }
         if constexpr (kAhead == 2) load_values(t + 2);

@@ -217,6 +217,19 @@ def test_values_that_are_not_finite_stay_in_their_dimension_and_behind_their_row
         assert torch.equal(out[:-1][..., [5, 9, 11]], clean[:-1][..., [5, 9, 11]])  # (those before it do not)
 
 
+@pytest.mark.parametrize("new,G", [([1], 4), ([4], 8), ([8], 8), ([100], 4)])
+def test_infinite_values_make_their_dimension_infinite(new, G):
+    b = Batch(new, [700], 1, 16)
+    clean = _attend(b, G)[1]
+    b.values[0][0, 10, 5], b.values[0][0, 300, 9], b.values[0][0, 300, 11] = math.inf, -math.inf, math.nan      # (older keys, which every row sees)
+    b.values[0][0, 20, 13], b.values[0][0, 21, 13] = math.inf, -math.inf
+    b.write()
+    out = b.paged().mp_paged_attention(_rows(b.T, G + 3, 11, 2.0)[:, 2:2 + G], max_new=new[0])
+    rest = [d for d in range(128) if d not in (5, 9, 11, 13)]
+    assert torch.equal(out[..., rest], clean[..., rest])
+    assert (out[..., 5] == math.inf).all() and (out[..., 9] == -math.inf).all() and out[..., [11, 13]].isnan().all()
+
+
 def test_rows_of_the_same_values_give_them_back():
     # the weights sum to one, whatever the split
     for new, lens in (([1], [30001]), ([3], [4001]), ([200], [3001])):
