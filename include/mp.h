@@ -472,7 +472,7 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
 /* mp_paged_attention -- every new token attends the keys of its sequence up to its own.
  *   q               device bf16 [n_tokens, n_q_heads, 128] with a token stride
  *   max_new         no sequence has more new tokens (rows past that are left as they were); 0: n_tokens.  It
- *                   says which kernels run: a decode step passes 1.
+ *                   says which kernels run, and how large the workspace is: a decode step passes 1.
  *   window          a token attends its last `window` keys, itself among them; 0: all
  *   softmax_scale   0 => 1/sqrt(128)
  *   out             device bf16 [n_tokens, n_q_heads, 128]
@@ -481,7 +481,10 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
  *                   max_new) bytes on a 16-byte boundary; it need not be cleared, and calls that may overlap on the GPU
  *                   need one each
  * A token that attends no key (position below zero, pages missing) gets zeros and -inf.  1 <= G <= 8.  fp32 accumulation
- * of bf16 products; probabilities are rounded to bf16 for their product with the values.
+ * of bf16 products; for their product with the values, probabilities are split into two bf16 parts (2^-17) where max_new * G <= 32, and
+ * for sequences of up to 16 query rows a KV head beside longer ones; otherwise they are rounded to bf16 (2^-9).  The denominator sums them
+ * in fp32.  What a token does not attend may hold anything: a value that is not finite reaches the tokens that attend it, in its dimension, and no others.
+ * Results do not depend on what runs beside the call, and repeat bit for bit for the same lengths and kernels.
  * Errors: MP_EINVAL, MP_EHIP. */
 size_t mp_paged_workspace_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t max_new);
 mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_stride, int32_t n_tokens,

@@ -11,8 +11,8 @@ namespace mp {
 namespace {
 
 // Which kernels a call runs.  That for few tokens takes sequences of up to `tokens` query rows a KV head (0: it does not run): as many as any sequence can
-// have, where it can.  Otherwise that for chunks runs, and the former takes the sequences of up to 16 rows, unless none need be there (one sequence, or as many tokens in the call
-// as its sequences can have).
+// have, where it can (64 rows each of 8 sequences of up to 30K keys: 103 us, by that for chunks 132).  Otherwise that for chunks runs, and the former takes the sequences of up
+// to 16 rows, unless none need be there (one sequence, or as many tokens in the call as its sequences can have); fifteen tokens beside 333 of a prompt: 151 us by that for chunks alone, 122 by both, when both were new.
 struct Kernels {
     int tokens;
     bool chunks;

@@ -4,7 +4,10 @@
 // 32 keys and values straight to LDS (global_load_lds, 16 bytes a lane, four rows an instruction) into a ring of two tiles, three of four
 // 8 KiB pieces on their way while one is used.  For 16 rows, S^T = K Q^T is eight v_mfma_f32_16x16x32_bf16 and O^T += V^T P^T as many: a lane holds one
 // query row of each 16 (its column) in both, and what it holds of S^T is what the second product takes of it.  Four waves with runs of tiles of their own make a workgroup,
-// whose sums meet in LDS; workgroups have equal shares of all sequences' keys (mp_paged_plan.h).
+// whose sums meet in LDS; workgroups have equal shares of all sequences' keys (mp_paged_plan.h), one a compute unit.
+//
+// One token each of 16 sequences of up to 128K keys, 8 KV heads of four: 592 us, 6.65 TB/s; 40 rows each of 8 sequences of up to 30K: 95 us, 5.1 TB/s; one
+// token over 4096 keys: 7.5 us and 4.5 for the merge, trips to memory one behind the other (lengths, page, keys, parts) and two launches.
 #include <type_traits>
 
 #include "mp_paged_plan.h"
@@ -195,7 +198,7 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
             }
         }
         // Probabilities are two bf16 values each where the products for that cost nothing (up to 32 rows): what truncation leaves of one is the second, an error of 2^-17.
-        // Four groups take them rounded to bf16 (2^-9).
+        // Four groups take them rounded to bf16 (2^-9): 40 rows over 30K keys, eight sequences, 95 us, with two values 104.
         constexpr bool kTwo = kGroups <= 2;
         bf16x8 p[kGroups], p2[kTwo ? kGroups : 1];
 #pragma unroll
