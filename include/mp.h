@@ -482,9 +482,9 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
  *                   need one each
  * A token that attends no key (position below zero, pages missing) gets zeros and -inf.  1 <= G <= 8.  fp32 accumulation
  * of bf16 products; for their product with the values, probabilities are split into two bf16 parts (2^-17) where max_new * G <= 32, and
- * for sequences of up to 16 query rows a KV head beside longer ones; otherwise they are rounded to bf16 (2^-9).  The denominator sums them
+ * in large batches for sequences of up to 16 query rows a KV head beside longer ones; otherwise they are rounded to bf16 (2^-9).  The denominator sums them
  * in fp32.  What a token does not attend may hold anything: a value that is not finite reaches the tokens that attend it, in its dimension, and no others.
- * Results do not depend on what runs beside the call, and repeat bit for bit for the same lengths and kernels.
+ * Results of the same batch repeat bit for bit.
  * Errors: MP_EINVAL, MP_EHIP. */
 size_t mp_paged_workspace_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t max_new);
 mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_stride, int32_t n_tokens,

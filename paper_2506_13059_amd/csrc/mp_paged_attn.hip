@@ -11,8 +11,8 @@ namespace mp {
 namespace {
 
 // Which kernels a call runs.  That for few tokens takes sequences of up to `tokens` query rows a KV head (0: it does not run): as many as any sequence can
-// have, where it can (64 rows each of 8 sequences of up to 30K keys: 103 us, by that for chunks 132).  Otherwise that for chunks runs, and the former takes the sequences of up
-// to 16 rows, unless none need be there (one sequence, or as many tokens in the call as its sequences can have); fifteen tokens beside 333 of a prompt: 151 us by that for chunks alone, 122 by both, when both were new.
+// have, where it can (8 sequences of up to 30K keys, 40 and 64 rows each: 95 and 107 us, by that for chunks 110 and 123; of up to 1000 keys equal).  Otherwise that
+// for chunks runs, and the former takes the sequences of up to 16 rows, unless none need be there (one sequence, or as many tokens in the call as its sequences can have).
 struct Kernels {
     int tokens;
     bool chunks;
@@ -23,6 +23,18 @@ Kernels kernels_of(int n_tokens, int group, int n_seqs, int max_new)
     for (int most = 16; most <= 64; most *= 2)
         if (rows <= most) return Kernels{most, false};
     return Kernels{n_seqs > 1 && (long long)n_seqs * max_new > n_tokens ? 16 : 0, true};
+}
+
+// Short sequences beside longer ones go to their own kernel if they can have this many rows of keys, all heads together: its two launches cost some 20 us and it reads keys
+// at 6.6 TB/s, where in the kernel for chunks a sequence's few rows keep one wave of eight busy.  Single tokens beside a piece of 333 tokens, 8 KV heads of four, us by both kernels
+// and by that for chunks alone: 15 sequences that see 1023 keys 64 and 45, 4096 keys 101 and 99 (0.5M rows), up to 16K 189 and 196 (2M); 63 of up to 4096 keys 122 and 142,
+// of up to 16K 394 and 497; 1 and 3 of up to 16K 142 and 132, 150 and 142.  Lengths are known on the device only: what the page table or the window allows stands for them.
+constexpr long long kOwnKernelRows = 3 << 18;
+
+bool short_ones_apart(const PagedAttention& a)
+{
+    const long long room = (long long)a.c.table_stride << a.c.page_shift;
+    return (a.c.n_seqs - 1) * (a.window > 0 && a.window < room ? a.window : room) >= kOwnKernelRows / a.c.n_kv;
 }
 
 }  // namespace
@@ -37,7 +49,8 @@ size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_s
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s)
 {
     if (a.n_tokens <= 0 || a.c.n_seqs <= 0) return hipSuccess;
-    const Kernels k = kernels_of(a.n_tokens, a.n_q_heads / a.c.n_kv, a.c.n_seqs, a.max_new);
+    Kernels k = kernels_of(a.n_tokens, a.n_q_heads / a.c.n_kv, a.c.n_seqs, a.max_new);
+    if (k.chunks && !short_ones_apart(a)) k.tokens = 0;
     float* room = a.partials;
     if (k.tokens) {
         const hipError_t e = launch_paged_tokens(a, k.tokens, room, s);

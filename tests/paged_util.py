@@ -36,13 +36,14 @@ def turn_bound(x, want, freqs, interleaved, amplitude=1.0):
 
 
 class Batch:
-    """Sequences of `new` tokens behind len - new older ones.  What no sequence holds of the cache is NaN, unused entries name no page."""
+    """Sequences of `new` tokens behind len - new older ones.  What no sequence holds of the cache is NaN, unused entries name no page.
+    `columns`: of the page table, at least."""
 
-    def __init__(self, new, lens, Hkv, page, seed=1, pad_front=0, pad_back=0, spare=2, stale=math.nan, scale=1.0):
+    def __init__(self, new, lens, Hkv, page, seed=1, pad_front=0, pad_back=0, spare=2, stale=math.nan, scale=1.0, columns=0):
         g = gen(seed)
         self.new, self.lens, self.Hkv, self.page = list(new), list(lens), Hkv, page
         n = [max(0, -(-k // page)) for k in lens]
-        width = max(n + [1]) + 1
+        width = max(max(n + [1]) + 1, columns)
         self.n_pages = sum(n) + spare
         order = torch.randperm(self.n_pages, generator=torch.Generator().manual_seed(seed)).tolist()
         table = torch.full((len(lens), width), -1, dtype=torch.int32)

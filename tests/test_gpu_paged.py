@@ -152,6 +152,21 @@ def test_attention_of_chunks(new, lens, G, page, Hkv, window):
     _attend(Batch(new, lens, Hkv, page, pad_front=3, pad_back=1), G * Hkv, window)
 
 
+@pytest.mark.parametrize("columns", [0, 8192], ids=["small", "room for long sequences"])
+@pytest.mark.parametrize("window", [0, 65])
+@pytest.mark.parametrize("G", [1, 4, 5, 8])
+def test_single_tokens_beside_a_prompt(G, window, columns):
+    """Sequences of few and of many new tokens in one call, pages missing, also where nothing in the batch is as long as its page table has room for."""
+    b = Batch([1, 90, 0, 1, 4, 1, 17, 1], [1, 190, 40, 513, 77, 0, 17, 130], 2, 64, seed=G, pad_front=2, pad_back=3, columns=columns)
+    b.table[3, 2], b.table[4, 0], b.table[7, 1] = -1, b.n_pages + 9, -5
+    _attend(b, 2 * G, window)
+
+
+def test_windows_of_many_single_tokens_beside_a_prompt():
+    b = Batch([1] * 40 + [60] + [1] * 29, [100 + 43 * i for i in range(70)], 12, 16, pad_back=1)
+    _attend(b, 12, window=1000)
+
+
 def test_many_sequences_of_several_tiles():
     n = [1 + (7 * i) % 90 for i in range(150)]
     _attend(Batch(n, [k + (31 * i) % 400 for i, k in enumerate(n)], 1, 16, pad_front=5, pad_back=9), 8)
