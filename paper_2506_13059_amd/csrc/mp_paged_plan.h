@@ -4,7 +4,7 @@
 // with the blocks of keys that some of them attend.  All items' blocks, head after head, sequence after sequence, are one line that is cut into equal
 // shares, a workgroup each: lengths are known on the device only, and one long sequence among short ones, or few rows over many keys,
 // come out even.  In front of its blocks an item has some places that stand for its beginning and end (the first loads, the results), so that shares of
-// many short items do not take longer (a prompt of 8192 in groups of five: 930 us without them, 783 with).  An item within a share is finished there; one that is cut leaves its parts (maximum, sum and weighted values, in fp32) in the
+// many short items do not take longer (a prompt of 8192 in groups of five: 813 us with one place, 751 with three).  An item within a share is finished there; one that is cut leaves its parts (maximum, sum and weighted values, in fp32) in the
 // workspace for the launch behind.
 #pragma once
 #include "mp_device.h"

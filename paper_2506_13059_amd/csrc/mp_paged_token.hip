@@ -6,8 +6,8 @@
 // query row of each 16 (its column) in both, and what it holds of S^T is what the second product takes of it.  Four waves with runs of tiles of their own make a workgroup,
 // whose sums meet in LDS; workgroups have equal shares of all sequences' keys (mp_paged_plan.h), one a compute unit.
 //
-// One token each of 16 sequences of up to 128K keys, 8 KV heads of four: 592 us, 6.65 TB/s; 40 rows each of 8 sequences of up to 30K: 95 us, 5.1 TB/s; one
-// token over 4096 keys: 7.5 us and 4.5 for the merge, trips to memory one behind the other (lengths, page, keys, parts) and two launches.
+// One token each of 16 sequences of up to 128K keys, 8 KV heads of four: 585 to 593 us, 6.6 to 6.7 TB/s; 40 rows each of 8 sequences of up to 30K: 95 us, 5.1 TB/s; one
+// token over 4096 keys: 8.0 us and 4.9 for the merge, trips to memory one behind the other (lengths, page, keys, parts) and two launches.
 #include <type_traits>
 
 #include "mp_paged_plan.h"
@@ -197,8 +197,8 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
                     for (int i = 0; i < 4; ++i) st.o[r][d][i] *= f;
             }
         }
-        // Probabilities are two bf16 values each where the products for that cost nothing (up to 32 rows): what truncation leaves of one is the second, an error of 2^-17.
-        // Four groups take them rounded to bf16 (2^-9): 40 rows over 30K keys, eight sequences, 95 us, with two values 104.
+        // Probabilities are two bf16 values each where the products for that cost nothing (up to 32 rows): what truncation leaves of one (2^-7) is the second, rounded (2^-8): an error of 2^-15.
+        // Four groups take them rounded to bf16 (2^-8): 40 rows over 30K keys, eight sequences, 95 us, with two values 104.
         constexpr bool kTwo = kGroups <= 2;
         bf16x8 p[kGroups], p2[kTwo ? kGroups : 1];
 #pragma unroll
