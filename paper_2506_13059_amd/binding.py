@@ -201,7 +201,7 @@ def _token_rows(t, name, device):
     if t.dtype is torch.bfloat16 and t.get_device() == device and t.dim() == 3:
         n, h, d = t.shape
         s0, s1, s2 = t.stride()
-        if d == 128 and s2 == 1 and (s1 == 128 or h <= 1):
+        if d == 128 and s2 == 1 and (s1 == 128 or h <= 1) and (n <= 1 or s0 >= h * 128):      # (a broadcast token's stride of 0 would mean densely packed)
             return n, h, s0 if n > 1 else 0
     _reject(f"{name}: bf16 [tokens, heads, 128] on the current device, each token's rows behind one another, expected, got {tuple(t.shape)} with strides {t.stride()} of "
             f"{t.dtype} on {t.device}")

@@ -228,3 +228,16 @@ def test_attention_refuses(mp):
         _refused(mp, call(ok, ws=None), "workspace")
     assert call(ok, T=0) == mp.MP_OK and call(_cache(mp, n_seqs=0)) == mp.MP_OK
     assert mp.mp_paged_workspace_bytes(2, 7, 2, 1, 1) == mp.mp_paged_workspace_bytes(-1, 8, 2, 1, 1) == mp.mp_paged_workspace_bytes(2, 18, 2, 1, 1) == 0
+
+
+def test_rows_that_lie_over_one_another_are_refused(mp):
+    """A broadcast token has no stride, which the library would take for densely packed rows: past the tensor's end."""
+    import torch
+    x = torch.zeros(1, 2, 128, dtype=torch.bfloat16)
+    for bad in (x.expand(4, 2, 128), torch.zeros(900, dtype=torch.bfloat16).as_strided((3, 2, 128), (128, 128, 1))):
+        with pytest.raises(mp.MpError) as e:
+            mp._token_rows(bad, "x", bad.get_device())
+        assert e.value.status == mp.MP_EINVAL
+    assert mp._token_rows(x, "x", x.get_device()) == (1, 2, 0)
+    assert mp._token_rows(x.expand(4, 2, 128).contiguous(), "x", x.get_device()) == (4, 2, 256)
+    assert mp._token_rows(torch.zeros(4, 5, 128, dtype=torch.bfloat16)[:, 1:3], "x", -1) == (4, 2, 640)
