@@ -460,7 +460,7 @@ typedef struct {
  * their queries in the same launch.
  *   rotary     NULL: keys (and queries) are stored as they come
  *   q, q_out   device bf16 [n_tokens, n_q_heads, 128], q with a token stride, q_out densely packed (it may be q if that is,
- *              too); both NULL: keys and values only
+ *              too, and overlaps nothing else); both NULL: keys and values only
  *   k, v       device bf16 [n_tokens, n_kv_heads, 128] with token strides
  *   n_tokens   rows of the tensors (>= q_start[n_seqs]; rows past that are not read)
  * Tokens at a negative position, behind the table's end or without a page are dropped (their queries are turned all the same).
@@ -475,7 +475,7 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
  *                   says which kernels run, and how large the workspace is: a decode step passes 1.
  *   window          a token attends its last `window` keys, itself among them; 0: all
  *   softmax_scale   0 => 1/sqrt(128)
- *   out             device bf16 [n_tokens, n_q_heads, 128]
+ *   out             device bf16 [n_tokens, n_q_heads, 128]; it does not lie between q's first and last row (MP_EINVAL), nor over any other argument
  *   lse             device fp32 [n_tokens, n_q_heads], natural log of the softmax denominator; may be NULL
  *   workspace       device buffer of at least mp_paged_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, n_seqs,
  *                   max_new) bytes on a 16-byte boundary; it need not be cleared, and calls that may overlap on the GPU

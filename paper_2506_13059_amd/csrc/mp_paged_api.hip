@@ -205,6 +205,10 @@ mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(nullptr, MP_EINVAL, "%s: workspace of %zu bytes, %zu are needed", who, workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned(workspace)) return fail(nullptr, MP_EINVAL, "%s: the workspace does not start on 16 bytes", who);
+    // (workgroups that share a tile of query rows read them until the last of them is done)
+    const uintptr_t q0 = (uintptr_t)q, q1 = q0 + 2 * ((uint64_t)(n_tokens - 1) * rows.stride + (uint64_t)n_q_heads * kHeadDimHost);
+    const uintptr_t o0 = (uintptr_t)out, o1 = o0 + 2 * (uint64_t)n_tokens * n_q_heads * kHeadDimHost;
+    if (o0 < q1 && q0 < o1) return fail(nullptr, MP_EINVAL, "%s: out overlaps the rows of q", who);
     a.q = rows.p;
     a.q_stride = rows.stride;
     a.n_tokens = n_tokens;
