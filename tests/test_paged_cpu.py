@@ -245,8 +245,10 @@ def test_rows_that_lie_over_one_another_are_refused(mp):
 
 def test_attention_does_not_write_over_its_queries(mp):
     """Workgroups that share a tile of rows read its queries until the last of them is done."""
+    cache = _cache(mp)
+
     def call(q, out, qs=0):
-        return mp.lib().mp_paged_attention(C.addressof(_cache(mp)), q, qs, 2, 8, 0, 0, 0.0, out, None, A, 1 << 40, None)
+        return mp.lib().mp_paged_attention(C.addressof(cache), q, qs, 2, 8, 0, 0, 0.0, out, None, A, 1 << 40, None)
     rows = 8 * 128 * 2
     for q, out, qs in ((A, A, 0), (A, A + 2 * rows - 16, 0), (A + 2 * rows - 16, A, 0), (A, A + 3 * rows, 8 * 128 * 4), (A, A + rows, 8 * 128 * 4)):
         _refused(mp, call(q, out, qs), "overlaps")
