@@ -484,7 +484,8 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
  * of bf16 products; for their product with the values, probabilities are split into two bf16 parts (2^-15) where max_new * G <= 32, and
  * in large batches for sequences of up to 16 query rows a KV head beside longer ones; otherwise they are rounded to bf16 (2^-8).  The denominator sums them
  * in fp32.  What a token does not attend may hold anything: a value that is not finite reaches the tokens that attend it, in its dimension, and no others.
- * Results of the same batch repeat bit for bit.
+ * Results of the same batch repeat bit for bit.  Calls whose new tokens, in tiles of 256 / G and one more a sequence, times the blocks of 64 keys that
+ * the page table has room for (or the window) come to 2^32 are refused.
  * Errors: MP_EINVAL, MP_EHIP. */
 size_t mp_paged_workspace_bytes(int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t max_new);
 mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_stride, int32_t n_tokens,

@@ -53,6 +53,7 @@ size_t paged_token_floats(int rows);
 hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s);
 size_t paged_chunk_floats();
 hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s);     // sequences of more than `over` query rows a head
+bool paged_line_fits(const PagedAttention& a);      // what the kernels count of a call's blocks stays within 32 bits
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s);
 
 // The sequence of token t: the last one that starts at or before it (sequences without new tokens start where the next one does), or -1

@@ -16,7 +16,10 @@ mp_status fail(mp_ctx* ctx, mp_status st, const char* fmt, ...);      // mp_api.
 
 namespace {
 
-constexpr long long kMostBlocks = 0x7fffffff;
+constexpr long long kMostKeys = 0x7fffffff;
+constexpr long long kMostRows = 4ll * 0x7fffffff;
+constexpr long long kMostGroups = (1ll << 24) - 1;      // workgroups of 256: a launch counts its lanes in 32 bits
+constexpr long long kMostTokens = 4 * kMostGroups;      // ... where every token has a wave
 
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -58,7 +61,7 @@ mp_status cache_ok(const char* who, const mp_paged_kv* c, PagedKv* out)
                     c->table_stride);
     if (c->page_size < 1 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
         return fail(nullptr, MP_EINVAL, "%s: page_size %d is not a power of two up to 1024", who, c->page_size);
-    if ((long long)c->table_stride * c->page_size > kMostBlocks)
+    if ((long long)c->table_stride * c->page_size > kMostKeys)
         return fail(nullptr, MP_EINVAL, "%s: a sequence's pages hold more than 2^31 - 1 keys", who);
     if (!c->k_pages || !c->v_pages) return fail(nullptr, MP_EINVAL, "%s: null pages", who);
     if (!aligned(c->k_pages) || !aligned(c->v_pages)) return fail(nullptr, MP_EINVAL, "%s: pages do not start on 16 bytes", who);
@@ -133,7 +136,7 @@ mp_status mp_rotary(const mp_rotary_spec* rotary, const void* x, int64_t x_strid
     if (out_lookup && !aligned(out_lookup)) return fail(nullptr, MP_EINVAL, "%s: out_lookup does not start on 16 bytes", who);
     if (out_lookup && (out_lookup == out || (out_lookup == x && in.stride != (int64_t)n_heads * kHeadDimHost)))
         return fail(nullptr, MP_EINVAL, "%s: out_lookup overlaps another tensor", who);
-    if (((long long)n_tokens * n_heads + 3) / 4 > kMostBlocks) return fail(nullptr, MP_EINVAL, "%s: too many rows", who);
+    if (n_tokens > kMostTokens || (long long)n_tokens * n_heads > kMostRows) return fail(nullptr, MP_EINVAL, "%s: too many rows", who);
     return launched(who, launch_rotary(rot, in, positions, n_tokens, (uint16_t*)out, to.stride, (uint16_t*)out_lookup, lookup_position, (hipStream_t)stream));
 }
 
@@ -158,7 +161,7 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
     }
     if ((st = rows_ok(who, "k", k, k_stride, c.n_kv, &tk)) != MP_OK) return st;
     if ((st = rows_ok(who, "v", v, v_stride, c.n_kv, &tv)) != MP_OK) return st;
-    if ((long long)n_tokens * (tq.n_heads + 2ll * c.n_kv) / 4 + 4 > kMostBlocks) return fail(nullptr, MP_EINVAL, "%s: too many rows", who);
+    if (n_tokens > kMostTokens || n_tokens * (tq.n_heads + 2ll * c.n_kv) > kMostRows) return fail(nullptr, MP_EINVAL, "%s: too many rows", who);
     return launched(who, launch_paged_append(c, rot, tq, (uint16_t*)q_out, tk, tv, n_tokens, (hipStream_t)stream));
 }
 
@@ -171,10 +174,10 @@ mp_status mp_paged_gather(const mp_paged_kv* cache, const mp_rotary_spec* rotary
     mp_status st = cache_ok(who, cache, &c);
     if (st != MP_OK) return st;
     if (k_lookup && (st = rotation_ok(who, rotary, &rot)) != MP_OK) return st;
-    if (first < 0 || n < 0 || (long long)first + n > kMostBlocks) return fail(nullptr, MP_EINVAL, "%s: bad range first=%d n=%d", who, first, n);
+    if (first < 0 || n < 0 || (long long)first + n > kMostKeys) return fail(nullptr, MP_EINVAL, "%s: bad range first=%d n=%d", who, first, n);
     if (!k && !k_lookup && !v) return fail(nullptr, MP_EINVAL, "%s: no output", who);
     if (!aligned(k) || !aligned(k_lookup) || !aligned(v)) return fail(nullptr, MP_EINVAL, "%s: an output does not start on 16 bytes", who);
-    if (((long long)n / 16 + 1) * c.n_seqs > kMostBlocks) return fail(nullptr, MP_EINVAL, "%s: too many rows", who);
+    if (((long long)n + 15) / 16 * c.n_seqs > kMostGroups) return fail(nullptr, MP_EINVAL, "%s: too many rows", who);
     return launched(who, launch_paged_gather(c, rot, first, n, lookup_position, (uint16_t*)k, (uint16_t*)k_lookup, (uint16_t*)v, (hipStream_t)stream));
 }
 
@@ -220,7 +223,7 @@ mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_
     a.out = (uint16_t*)out;
     a.lse = lse;
     a.partials = (float*)workspace;
-    if (((long long)n_tokens * n_q_heads + 3) / 4 > kMostBlocks) return fail(nullptr, MP_EINVAL, "%s: too many rows", who);
+    if (!paged_line_fits(a)) return fail(nullptr, MP_EINVAL, "%s: too many tokens over a page table with room for so many keys", who);
     return launched(who, launch_paged_attention(a, (hipStream_t)stream));
 }
 

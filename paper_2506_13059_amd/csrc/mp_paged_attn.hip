@@ -46,6 +46,15 @@ size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_s
     return (k.tokens ? paged_token_floats(k.tokens) : 0) + (k.chunks ? paged_chunk_floats() : 0);
 }
 
+// A head's blocks on the line (mp_paged_plan.h) at most, in the kernel that has the smaller tiles, blocks and more places in front; tiles: what all tokens fill, and one that is not full a sequence.
+bool paged_line_fits(const PagedAttention& a)
+{
+    const long long tokens = 256 / (a.n_q_heads / a.c.n_kv), room = (long long)a.c.table_stride << a.c.page_shift;
+    const long long keys = a.window > 0 && a.window + tokens < room ? a.window + tokens : room;
+    const long long tiles = a.n_tokens / tokens + (a.c.n_seqs < a.n_tokens ? a.c.n_seqs : a.n_tokens);
+    return tiles * (keys / 64 + 5) < 1ll << 32;
+}
+
 hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s)
 {
     if (a.n_tokens <= 0 || a.c.n_seqs <= 0) return hipSuccess;

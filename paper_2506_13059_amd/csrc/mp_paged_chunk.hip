@@ -430,7 +430,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         const int key = t * kKeys + __ffsll((long long)odd) - 1;
                         const int page = __builtin_amdgcn_readfirstlane(page_of(entries, a.c.table_stride, a.c.n_pages, a.c.page_shift, key));
                         const bool sees = key <= position && !(a.window && key <= position - a.window);
-                        const uint2* from = reinterpret_cast<const uint2*>(a.c.V + row_of(page, h, a.c.n_kv, a.c.page_shift, key) * kHeadDim);
+                        const uint2* from = reinterpret_cast<const uint2*>(a.c.V + row_of(max(page, 0), h, a.c.n_kv, a.c.page_shift, key) * kHeadDim);
 #pragma unroll
                         for (int d = 0; d < 4; ++d)
 #pragma unroll

@@ -154,7 +154,7 @@ struct Line {
     int s0, b0, b1;
     uint32_t before, total, incl;
 };
-// x / d (a line of 2^32 places or more is possible in principle only)
+// x / d (a head has fewer than 2^32 places, all of them together mostly)
 __device__ __forceinline__ long long quotient(long long x, long long d)
 {
     return ((x | d) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;

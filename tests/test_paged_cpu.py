@@ -252,3 +252,21 @@ def test_attention_does_not_write_over_its_queries(mp):
     rows = 8 * 128 * 2
     for q, out, qs in ((A, A, 0), (A, A + 2 * rows - 16, 0), (A + 2 * rows - 16, A, 0), (A, A + 3 * rows, 8 * 128 * 4), (A, A + rows, 8 * 128 * 4)):
         _refused(mp, call(q, out, qs), "overlaps")
+
+
+def test_launches_and_lines_that_pass_their_counters_are_refused(mp):
+    """A launch counts its lanes and a line of blocks its places in 32 bits."""
+    spec, wide = _spec(mp), _cache(mp, page_size=1024, table_stride=(1 << 21) - 1)
+    many = 1 << 27
+    _refused(mp, mp.lib().mp_rotary(C.addressof(spec), A, 0, A, many, 1, A, 0, None, 0, None), "too many")
+    cache = _cache(mp)
+    _refused(mp, mp.lib().mp_paged_append(C.addressof(cache), None, None, 0, 0, None, A, 0, A, 0, many, None), "too many")
+    lots = _cache(mp, n_seqs=1 << 20)
+    _refused(mp, mp.lib().mp_paged_gather(C.addressof(lots), None, 0, 4096, 0, A, None, A, None), "too many")
+    out = A + (1 << 50)
+    attend = lambda c, T, hq, most=0, window=0: mp.lib().mp_paged_attention(C.addressof(c), A, 0, T, hq, most, window, 0.0, out, None, A, 1 << 40, None)      # noqa: E731
+    _refused(mp, attend(wide, 1 << 20, 16), "too many")                                         # 2^31 keys under each of 2^15 tiles
+    for kw in (dict(n_seqs=1 << 17), dict(n_seqs=1 << 20)):                                     # 2^31 keys of each of many sequences
+        c = _cache(mp, page_size=1024, table_stride=(1 << 21) - 1, **kw)
+        _refused(mp, attend(c, kw["n_seqs"], 2, 1), "too many")
+    _refused(mp, attend(wide, 1 << 20, 16, window=1 << 30), "too many")
