@@ -5,7 +5,7 @@
 // needs no more of other lanes than one exchange of maxima, and the rows of S^T that it holds are, converted to bf16, what the second product takes from it,
 // with the values' rows read (transposed by LDS) in the same order.
 //
-// Bound by the matrix cores, and by what a chip at its power limit gives them: 2048 tokens at 128K, 32 heads, 4.1 to 4.3 ms = 1.02 to 1.06 PFLOP/s at 2.0 to 2.1 GHz, from
+// Bound by the matrix cores, and by what a chip at its power limit gives them: 2048 tokens at 128K, 32 heads, 4.1 to 4.35 ms = 1.0 to 1.06 PFLOP/s at 2.0 to 2.1 GHz, from
 // card to card (a large library product: 1.35 to 1.39 PFLOP/s); the cores are busy 49 % of the cycles, the vector ALU with exponentials, sums, maxima and conversions (about
 // 175 instructions a block and wave) 46 %, both as counted.  Eight waves, so that each SIMD has two: one computes where the other waits.  What brought it there, the same call: rows
 // through registers, one block ahead 5.03 ms; straight to LDS 4.73; loads among the products 4.46; cheaper shares and page entries 4.35; waves that meet every second block 4.31; maxima 4.20 -> 4.12.

@@ -7,7 +7,7 @@
 // All three are copies that rotate on the way: bound by memory, or by a launch and two trips to memory where there are few tokens.  A
 // row is 16 lanes of 16 bytes.  Sines and cosines of a position are worked out once a wave (one pair a lane) or workgroup and serve all of its
 // heads from LDS; a lane's partner elements of the half layout come from another lane's registers.  A decode step's calls take 4.4 to 4.8 us on the device; 8191 tokens' 40
-// query heads 34 us (5.0 TB/s read and written), five prompts' append 94 us (5.2 TB/s), the gather of four sequences of 64K with lookup keys 509 us (5.3 TB/s).
+// query heads 34 us (4.9 TB/s read and written), five prompts' append 94 us (5.2 TB/s), the gather of four sequences of 64K with lookup keys 509 us (5.3 TB/s).
 #include "mp_device.h"
 #include "mp_paged.h"
 
