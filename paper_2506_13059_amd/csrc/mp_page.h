@@ -25,6 +25,14 @@ MP_PAGE_FN long long row_of(int page, int head, int n_kv, int page_shift, int po
     return (((long long)page * n_kv + head) << page_shift) + (position & ((1 << page_shift) - 1));
 }
 
+// The entry of key unit * block + offset in a sequence's row of the table; behind its `end` keys (one at least), that of the last one.  Blocks that are asked for
+// ahead may lie up to 2^31 keys behind the end, so the key is worked out in unsigned numbers.
+MP_PAGE_FN int entry_of(int block, int unit, int offset, int end, int page_shift)
+{
+    const uint32_t key = (uint32_t)block * (uint32_t)unit + (uint32_t)offset, last = (uint32_t)end - 1u;
+    return (int)((key < last ? key : last) >> page_shift);
+}
+
 // Blocks of `unit` keys that tokens [i0, i1] of a sequence attend (token i stands at position base + i): [b0, b1), one at least, so that
 // rows without a key are someone's, too.  `room`: keys that the table has entries for.
 MP_PAGE_FN void blocks_of(int base, int i0, int i1, int window, int room, int unit, int* b0, int* b1)

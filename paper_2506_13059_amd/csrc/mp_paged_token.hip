@@ -68,7 +68,7 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
     const uint32_t v_at = ring + kPiece + (uint32_t)(vr * 256 + ((((col & 3) >> 1) ^ ((vr & 7) << 1)) << 4) + (col & 1) * 8);      // ^ 32 d
 
     // (entries are looked at two tiles after they were asked for: looked at at once, they made the wave wait for all loads before them)
-    auto entry_at = [&](int t) { return c.entries[min(t * kTile + (kOnePage ? lane & 16 : lane & 31), c.end - 1) >> c.shift]; };      // of key 32 t + lane % 32, or of its half
+    auto entry_at = [&](int t) { return c.entries[entry_of(t, kTile, kOnePage ? lane & 16 : lane & 31, c.end, c.shift)]; };      // of key 32 t + lane % 32, or of its half
     auto held = [&](int t, int entry) {
         if constexpr (kOnePage) {
             const int n = c.end - t * kTile;
