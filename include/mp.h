@@ -480,7 +480,8 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
  *   workspace       device buffer of at least mp_paged_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, n_seqs,
  *                   max_new) bytes on a 16-byte boundary; it need not be cleared, and calls that may overlap on the GPU
  *                   need one each
- * A token that attends no key (position below zero, pages missing) gets zeros and -inf.  1 <= G <= 8.  fp32 accumulation
+ * A token that attends no key (position below zero, pages missing) gets zeros and -inf, and so does one all of whose logits are -inf.  A logit of NaN or +inf
+ * makes its token's row of that head NaN, lse too.  1 <= G <= 8.  fp32 accumulation
  * of bf16 products; for their product with the values, probabilities are split into two bf16 parts (2^-15) where max_new * G <= 32, and
  * in large batches for sequences of up to 16 query rows a KV head beside longer ones; otherwise they are rounded to bf16 (2^-8).  The denominator sums them
  * in fp32.  What a token does not attend may hold anything: a value that is not finite reaches the tokens that attend it, in its dimension, and no others.

@@ -114,18 +114,19 @@ __device__ __forceinline__ void lds_write1(uint32_t at, uint32_t v) { asm volati
 // The lowest n of 64 bits.
 __device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 
-__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY; }
+// (a denominator of 0: no key, or none of any weight; NaN, of a logit that is NaN or +inf, stays)
+__device__ __forceinline__ float lse_of(float m, float l) { return l != 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY; }
 
 // A lane's dims 32 d + 8 j + 4 half .. of a finished row, o[j] over l.
 __device__ __forceinline__ void store_dims(const PagedAttention& a, long long row, int d, int half, const f32x4 (&o)[4], float l)
 {
-    const float f = l > 0.f ? 1.f / l : 0.f;
+    const float f = l != 0.f ? 1.f / l : 0.f;
     unsigned char* out = reinterpret_cast<unsigned char*>(a.out) + row * 256 + half * 8 + d * 64;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         bf16x4 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (__bf16)(l > 0.f ? o[j][e] * f : 0.f);
+        for (int e = 0; e < 4; ++e) w[e] = (__bf16)(l != 0.f ? o[j][e] * f : 0.f);
         *reinterpret_cast<bf16x4*>(out + j * 16) = w;
     }
 }

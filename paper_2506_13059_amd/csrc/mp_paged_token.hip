@@ -299,13 +299,14 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
 
 __device__ __forceinline__ void store_row(const PagedAttention& a, int token, int head, const f32x4& o, float m, float l, int d, int g)
 {
-    const float f = l > 0.f ? 1.f / l : 0.f;
+    const bool some = l != 0.f;              // (0: no key, or none of any weight; NaN, of a logit that is NaN or +inf, stays)
+    const float f = some ? 1.f / l : 0.f;
     const long long row = (long long)token * a.n_q_heads + head;
     bf16x4 w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = (__bf16)(l > 0.f ? o[e] * f : 0.f);
+    for (int e = 0; e < 4; ++e) w[e] = (__bf16)(some ? o[e] * f : 0.f);
     *reinterpret_cast<bf16x4*>(a.out + row * kHeadDim + 16 * d + 4 * g) = w;
-    if (a.lse && d == 0 && g == 0) a.lse[row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+    if (a.lse && d == 0 && g == 0) a.lse[row] = some ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
 }
 
 template <int kGroups, bool kOnePage>
