@@ -104,13 +104,18 @@ __device__ __forceinline__ void partners(const uint4& w, const Turn& t, const Ro
     }
 }
 
+// (dims that are not turned keep their bits: no 0 * inf, and no NaN made another one)
 __device__ __forceinline__ uint4 turned(const uint4& w, const float (&y)[8], const Turn& t)
 {
     float x[8];
     unpack(w, x);
+    uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < t.n ? fmaf(y[i], t.sn[i], x[i] * t.cs[i]) : x[i];     // (no 0 * inf in the rest)
-    return make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+    for (int i = 0; i < 4; ++i) {        // (rot_dim is even: both dims of a word, or neither)
+        const uint32_t r = pack2(fmaf(y[2 * i], t.sn[2 * i], x[2 * i] * t.cs[2 * i]), fmaf(y[2 * i + 1], t.sn[2 * i + 1], x[2 * i + 1] * t.cs[2 * i + 1]));
+        u[i] = 2 * i < t.n ? r : u[i];
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
 // Cosines and sines of one position for a wave, in its part of LDS.
