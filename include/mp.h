@@ -440,8 +440,9 @@ mp_status mp_rotary(const mp_rotary_spec* rotary, const void* x, int64_t x_strid
  * appended rows for it are dropped, gathered rows of it are zero.  Sequences may share pages that are only read.
  * The new tokens of a call are the rows [q_start[b], q_start[b+1]) of its tensors for sequence b (q_start does not decrease); they are the
  * last ones of its kv_len[b] keys, so token i of n stands at position kv_len[b] - n + i.  Rows before q_start[0] and
- * behind q_start[n_seqs] belong to no sequence: their outputs are left as they were.  Nothing else is ever read of the
- * pages than the rows of kv_len[b] keys; the rest of a page may hold anything. */
+ * behind q_start[n_seqs] belong to no sequence: their outputs are left as they were.  Results depend on no
+ * other rows of the pages than those of kv_len[b] keys, so the rest of a page may hold anything; but attention loads whole blocks of keys, and in the place of keys that
+ * are not there rows of page 0: any row of the n_pages pages may be read, and has to be memory that can be. */
 typedef struct {
     void* k_pages;               /* device bf16 [n_pages, n_kv_heads, page_size, 128]                 */
     void* v_pages;               /* likewise                                                          */
