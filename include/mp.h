@@ -496,6 +496,8 @@ mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_
 
 /* mp_paged_gather -- keys and values [first, first + n) of every sequence in order; rows that a sequence does not hold are
  * zero.  q_start is not used.
+ * mp_cluster_kv and mp_local_buffer_init take as many tokens of every sequence, and a zero row would be a key to them, with logits of zero.  Sequences of different lengths are
+ * gathered and indexed a length at a time: n_seqs sequences from b on are the cache with page_table + b * table_stride, kv_len + b and q_start + b.
  *   k, k_lookup, v   device bf16 [n_seqs, n_kv_heads, n, 128]; each may be NULL, one is not
  *   k_lookup         the stored keys turned on from their position to lookup_position, without another amplitude
  *                    (`rotary`: what they were stored with; it may be NULL without k_lookup)

@@ -340,7 +340,8 @@ class MpPagedKv:
         return out
 
     def mp_paged_gather(self, n, first=0, rotary=None, lookup_position=None, k=None, v=None, k_lookup=None):
-        """Keys and values [first, first + n) of every sequence: (k, v) bf16 [n_seqs, Hkv, n, 128], with a lookup_position (k, v, k_lookup)."""
+        """Keys and values [first, first + n) of every sequence: (k, v) bf16 [n_seqs, Hkv, n, 128], with a lookup_position (k, v, k_lookup).  Rows that a
+        sequence does not hold are zero, and would be keys to mp_cluster_kv: gather sequences of other lengths through an MpPagedKv of their own (page_table[b:b + 1], ...)."""
         device = self._current()
         if n < 0:
             _reject(f"n = {n} < 0")
