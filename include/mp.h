@@ -416,6 +416,7 @@ typedef struct {
  *   MP_ROTARY_BASE      the plain ones of base * factor^(rot_dim / (rot_dim - 2))
  *   MP_ROTARY_BY_PARTS  a pair that turns r = original_len f_i / 2 pi times over the original length keeps the share
  *                       g = clamp((r - low) / (high - low), 0, 1) of its frequency: g f_i + (1 - g) f_i / factor
+ * By parts, the share goes by a pair's turns; frequencies that go by its number instead, or by a table of their own, are put into mp_rotary_spec as they are.
  * Arguments that a scaling does not name are ignored.  Errors: MP_EINVAL. */
 #define MP_ROTARY_PLAIN 0
 #define MP_ROTARY_LINEAR 1
@@ -473,14 +474,16 @@ mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary
 /* mp_paged_attention -- every new token attends the keys of its sequence up to its own.
  *   q               device bf16 [n_tokens, n_q_heads, 128] with a token stride
  *   max_new         no sequence has more new tokens (rows past that are left as they were); 0: n_tokens.  It
- *                   says which kernels run, and how large the workspace is: a decode step passes 1.
+ *                   says which kernels run, and how large the workspace is: a decode step passes 1 (as many as its tokens instead, 16 of
+ *                   them over 4096 keys each take 58 us for 50, and their probabilities one part for two, see below).
  *   window          a token attends its last `window` keys, itself among them; 0: all
  *   softmax_scale   0 => 1/sqrt(128)
  *   out             device bf16 [n_tokens, n_q_heads, 128]; it does not lie between q's first and last row (MP_EINVAL), nor over any other argument
  *   lse             device fp32 [n_tokens, n_q_heads], natural log of the softmax denominator; may be NULL
  *   workspace       device buffer of at least mp_paged_workspace_bytes(n_tokens, n_q_heads, n_kv_heads, n_seqs,
  *                   max_new) bytes on a 16-byte boundary; it need not be cleared, and calls that may overlap on the GPU
- *                   need one each
+ *                   need one each.  4, 8 or 16 MiB for max_new * G up to 16, 32 and 64, otherwise 65, or 69 where some sequences may have
+ *                   few new tokens; whatever the lengths
  * A token that attends no key (position below zero, pages missing) gets zeros and -inf, and so does one all of whose logits are -inf.  A logit of NaN or +inf
  * makes its token's row of that head NaN, lse too.  1 <= G <= 8.  fp32 accumulation
  * of bf16 products; for their product with the values, probabilities are split into two bf16 parts (2^-15) where max_new * G <= 32, and

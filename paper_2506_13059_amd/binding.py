@@ -320,7 +320,9 @@ class MpPagedKv:
         return q_out
 
     def mp_paged_attention(self, q, max_new=0, window=0, softmax_scale=0.0, out=None, lse=None, workspace=None):
-        """q bf16 [tokens, Hq, 128] -> out bf16 [tokens, Hq, 128] (and lse fp32 [tokens, Hq]); max_new: as many new tokens a sequence at most."""
+        """q bf16 [tokens, Hq, 128] -> out bf16 [tokens, Hq, 128] (and lse fp32 [tokens, Hq]); max_new: as many new tokens a sequence at most.  0 stands for
+        as many as q has: a decode step passes 1, which takes the kernel for it, probabilities in two bf16 parts and 4 MiB of workspace.  Without a workspace one is
+        allocated (up to 69 MiB)."""
         device = self._current()
         n, hq, qs = _token_rows(q, "q", device)
         if out is None:

@@ -25,10 +25,11 @@ Kernels kernels_of(int n_tokens, int group, int n_seqs, int max_new)
     return Kernels{n_seqs > 1 && (long long)n_seqs * max_new > n_tokens ? 16 : 0, true};
 }
 
-// Short sequences beside longer ones go to their own kernel if they can have this many rows of keys, all heads together: its two launches cost some 20 us and it reads keys
+// Short sequences beside longer ones go to their own kernel if they can have this many rows of keys, all heads together: its two launches cost 8 to 13 us and it reads keys
 // at 6.6 TB/s, where in the kernel for chunks a sequence's few rows keep one wave of eight busy.  Single tokens beside a piece of 333 tokens, 8 KV heads of four, us by both kernels
-// and by that for chunks alone: 15 sequences that see 1023 keys 64 and 45, 4096 keys 101 and 99 (0.5M rows), up to 16K 189 and 196 (2M); 63 of up to 4096 keys 122 and 142,
-// of up to 16K 394 and 497; 1 and 3 of up to 16K 142 and 132, 150 and 142.  Lengths are known on the device only: what the page table or the window allows stands for them.
+// and by that for chunks alone: 15 sequences that see 1023 keys 54 and 43, 4096 keys 94 and 97 (0.5M rows), a window of 4096 in 16K 98 and 101, up to 16K 153 and 172 (2M); 63 of up
+// to 4096 keys 113 and 136, of up to 16K 326 and 438; 1 and 3 of up to 16K 136 and 123, 135 and 127.  Lengths are known on the device only: what the page table or the window allows
+// stands for them, so a table with room for much more than its sequences hold costs them those 8 to 13 us.
 constexpr long long kOwnKernelRows = 3 << 18;
 
 bool short_ones_apart(const PagedAttention& a)

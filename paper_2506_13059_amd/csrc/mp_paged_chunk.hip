@@ -5,8 +5,8 @@
 // needs no more of other lanes than one exchange of maxima, and the rows of S^T that it holds are, converted to bf16, what the second product takes from it,
 // with the values' rows read (transposed by LDS) in the same order.
 //
-// Bound by the matrix cores, and by what a chip at its power limit gives them: 2048 tokens at 128K, 32 heads, 4.1 to 4.35 ms = 1.0 to 1.06 PFLOP/s at 2.0 to 2.1 GHz, from
-// card to card (a large library product: 1.35 to 1.39 PFLOP/s); the cores are busy 49 % of the cycles, the vector ALU with exponentials, sums, maxima and conversions (about
+// Bound by the matrix cores, at the clock that the power limit leaves (1370 of 1400 W read while it ran): 2048 tokens at 128K, 32 heads, 4.1 to 4.6 ms = 0.95 to 1.06 PFLOP/s at 2.0 to
+// 2.1 GHz, from card to card (a large library product: 1.35 to 1.39 PFLOP/s at 1.8 GHz); the cores are busy 49 % of the cycles, the vector ALU with exponentials, sums, maxima and conversions (about
 // 175 instructions a block and wave) 46 %, both as counted.  Eight waves, so that each SIMD has two: one computes where the other waits.  What brought it there, the same call: rows
 // through registers, one block ahead 5.03 ms; straight to LDS 4.73; loads among the products 4.46; cheaper shares and page entries 4.35; waves that meet every second block 4.31; maxima 4.20 -> 4.12.
 // Did nothing: waves of a SIMD half a block apart, priorities, more reads ahead.
@@ -163,7 +163,7 @@ __device__ __forceinline__ void store_part(float* part, const Softmax& st, float
     }
 }
 
-// kOnePage: pages of eight rows or more.
+// kOnePage: pages of eight rows or more.  (Smaller ones take addresses a lane, and eight registers more than there are: 2048 tokens at 32K 1.06 ms for 1.02.)
 template <bool kOnePage>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
 {
@@ -404,7 +404,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                         for (int j = 0; j < 16; ++j) st.o[d][j] *= f;
                 }
                 const float m = st.m == -INFINITY ? 0.f : st.m;
-                // Probabilities of 16 keys at a time, two elements behind each product of the 16 keys before.
+                // Probabilities of 16 keys at a time, two elements behind each product of the 16 keys before.  Each is rounded to bf16 once (2^-8, as much as the results are). In two
+                // parts (2^-15, as for single tokens) they take half as many products again: 2048 tokens at 128K 5.64 ms for 4.24, a prompt of 8192 in groups of five 0.93 for 0.74,
+                // fifteen tokens beside 333 of a prompt 116 us for 98.
                 bf16x8 p[4];
                 auto probabilities = [&](int k, int e) {
 #pragma unroll
