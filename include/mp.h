@@ -388,6 +388,9 @@ mp_status mp_dense_attention_static(const void* q, const void* k, const void* v,
  *   mp_paged_attention   the new tokens attend all that the cache holds of their sequence
  *   mp_paged_gather      a sequence's rows in order: what mp_cluster_kv and mp_local_buffer_init take
  *   mp_rotary            rotary positions by themselves: what mp_decode_step takes per token
+ *   mp_norm_rotary, mp_paged_append_norm   the same with a norm of every head's queries and keys before the rotation
+ *   mp_paged_reserve     page tables, lengths and starts of the next step, made on the device
+ *   mp_paged_tree_plan, mp_paged_tree_attention, mp_paged_tree_keep   drafted tokens that form a tree
  *
  * All are context-free (errors through mp_last_error(NULL)), run on the current device, allocate
  * nothing, wait for nothing and read nothing back.  Their kernels take lengths, starts and page
@@ -436,6 +439,21 @@ mp_status mp_rotary(const mp_rotary_spec* rotary, const void* x, int64_t x_strid
                     int32_t n_tokens, int32_t n_heads, void* out, int64_t out_stride, void* out_lookup,
                     int32_t lookup_position, void* stream);
 
+/* Norm of a head's rows: x / sqrt(mean(x^2) + eps) * (weight + offset), the mean over the row's 128 elements.  Worked out in fp32 with what follows it, and rounded to bf16 once.
+ * A row whose squares' sum passes fp32 (elements from 1.6e18 on) may be zero; one with an infinity is NaN in that element and its partner of the rotation, and zero elsewhere; one with a NaN
+ * is NaN. */
+typedef struct {
+    const void* weight;    /* device bf16 [n_heads, 128]                                              */
+    int32_t n_heads;       /* heads of the rows, or 1: the same weights for all of them               */
+    float offset;          /* 0, or 1 where weights are kept as what they differ from one by; finite  */
+    float eps;             /* above 0, finite                                                         */
+} mp_head_norm;
+
+/* mp_norm_rotary -- mp_rotary of normed rows: arguments, overlaps and errors as there; also MP_EINVAL for a bad norm. */
+mp_status mp_norm_rotary(const mp_head_norm* norm, const mp_rotary_spec* rotary, const void* x, int64_t x_stride, const int32_t* positions,
+                         int32_t n_tokens, int32_t n_heads, void* out, int64_t out_stride, void* out_lookup, int32_t lookup_position,
+                         void* stream);
+
 /* The paged cache and a batch of sequences over it.  Key j of sequence b lies in row j % page_size of page
  * page_table[b][j / page_size].  An entry outside [0, n_pages) stands for no page: its keys are attended by no one,
  * appended rows for it are dropped, gathered rows of it are zero.  Sequences may share pages that are only read.
@@ -470,6 +488,15 @@ typedef struct {
 mp_status mp_paged_append(const mp_paged_kv* cache, const mp_rotary_spec* rotary, const void* q, int64_t q_stride,
                           int32_t n_q_heads, void* q_out, const void* k, int64_t k_stride, const void* v,
                           int64_t v_stride, int32_t n_tokens, void* stream);
+
+/* mp_paged_append_norm -- mp_paged_append with norms of queries and keys before the rotation, and with positions of their own for the rotation.
+ *   q_norm, k_norm   either may be NULL: those rows are not normed.  q_norm is not looked at without q
+ *   positions        device int32 [n_tokens], what queries and keys are turned to (a tree's tokens stand behind one another in the cache, while their positions go by
+ *                    their paths); NULL: where they stand in their sequences.  Places in the cache are those of mp_paged_append in any case
+ * rotary may be NULL (norms alone).  Errors: MP_EINVAL, MP_EHIP. */
+mp_status mp_paged_append_norm(const mp_paged_kv* cache, const mp_rotary_spec* rotary, const mp_head_norm* q_norm, const mp_head_norm* k_norm,
+                               const int32_t* positions, const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, int32_t n_tokens, void* stream);
 
 /* mp_paged_attention -- every new token attends the keys of its sequence up to its own.
  *   q               device bf16 [n_tokens, n_q_heads, 128] with a token stride
@@ -507,6 +534,62 @@ mp_status mp_paged_attention(const mp_paged_kv* cache, const void* q, int64_t q_
  * Errors: MP_EINVAL, MP_EHIP. */
 mp_status mp_paged_gather(const mp_paged_kv* cache, const mp_rotary_spec* rotary, int32_t first, int32_t n,
                           int32_t lookup_position, void* k, void* k_lookup, void* v, void* stream);
+
+/* Page tables and what a step's tokens are, made on the device: a pool of pages beside the arrays that mp_paged_kv describes (the same addresses; all are changed in
+ * place, so a captured step follows them without the host).  free_pages is a stack: its first n_free[0] entries are pages in no use.  An entry of the table behind a sequence's keys is
+ * not looked at.  A page belongs to one sequence: for pages that sequences share, give the pool tables without them. */
+typedef struct {
+    int32_t* page_table;         /* device int32 [n_seqs, table_stride]                               */
+    int32_t* kv_len;             /* device int32 [n_seqs]                                             */
+    int32_t* q_start;            /* device int32 [n_seqs + 1], written                                */
+    int32_t* free_pages;         /* device int32 [n_pages]                                            */
+    int32_t* n_free;             /* device int32 [1]                                                  */
+    int32_t n_pages;             /* times page_size below 2^31                                        */
+    int32_t page_size;           /* a power of two, 1 .. 1024                                         */
+    int32_t n_seqs;
+    int32_t table_stride;        /* times page_size, and times n_seqs, below 2^31                     */
+} mp_page_pool;
+
+/* mp_paged_reserve -- one step of every sequence: keys that go, tokens that come.
+ *   n_new       device int32 [n_seqs], tokens to come (below 0: 0)
+ *   keep        device int32 [n_seqs], keys that stay, the first ones: kv_len (all) at most; 0 for a sequence that has ended; NULL: all
+ *   granted     device int32 [n_seqs] or NULL: tokens that have room, n_new or 0
+ *   sequence, positions, slots   device int32, int32, int64 [n_rows], each may be NULL: of every row of the step's tokens, its sequence, its position, and its row of the pages
+ *               (page * page_size + row); rows behind the last sequence get -1, and so do slots without a page.  Rows past n_rows are not described.
+ * The pages of entries [ceil(keep / page_size), ceil(kv_len / page_size)) go back on the stack, sequence after sequence, entry after entry, and the entries become -1 (entries outside
+ * [0, n_pages) have no page to give).  Then each sequence, in order, takes pages for its keys that stay and its tokens from the stack's top.  Where these are too few, that
+ * sequence and all behind it that need a page get no tokens (a sequence whose last page has room for its tokens gets them); nor does one whose table has no room.
+ * Places of the stack that were taken become -1.  Then kv_len = keep + granted, and q_start is the running sum of granted.
+ * The same arrays in give the same ones out.  n_new and keep are not results of the same call.  Errors: MP_EINVAL, MP_EHIP. */
+mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const int32_t* keep, int32_t* granted, int32_t* sequence,
+                           int32_t* positions, int64_t* slots, int32_t n_rows, void* stream);
+
+/* Trees of drafted tokens.  The new tokens of a sequence (see mp_paged_kv) form a tree, or several: each follows another new one, its parent, which stands
+ * before it, or the sequence's older keys.  Bit i % 64 of word i / 64 of a token's mask (mask_words words of 64 bits a token, 1 .. 16) marks new token i of
+ * its sequence.  New tokens from 64 * mask_words on are marked by no one.
+ *
+ * mp_paged_tree_plan -- masks and positions from parents.
+ *   parents     device int32 [n_tokens]: the parent's number among the new tokens of its sequence; anything that is no token before it: none
+ *   mask        device uint64 [n_tokens, mask_words]: the token and its ancestors
+ *   positions   device int32 [n_tokens]: kv_len - n + (ancestors), with n new tokens: what mp_paged_append_norm turns a token to
+ * Of a sequence, the first 64 * mask_words new tokens have results; other rows are left as they were.  The pages are not looked at.  Errors: MP_EINVAL, MP_EHIP.
+ *
+ * mp_paged_tree_attention -- every new token attends the keys of its sequence that are older than the new ones, and the new ones that its mask marks (any, also
+ * such as stand behind it; itself only if it is marked).  window: of all these, the last `window` keys.  Other arguments, workspace, results and errors as of mp_paged_attention.
+ *
+ * mp_paged_tree_keep -- the rows of an accepted path moved together: of every sequence, the new tokens that the mask of its new token leaf[b] marks become the first of the new
+ * ones, in their order, keys and values.  Rows without a page, before or after, are not moved; the rest of the rows is left as it was.
+ *   mask        as above, [n_tokens, mask_words]
+ *   leaf        device int32 [n_seqs], the last accepted one among the new tokens of its sequence; anything else (or one that has no mask): none is accepted
+ *   keep        device int32 [n_seqs]: kv_len - n + (marked tokens), what mp_paged_reserve keeps in the next step; kv_len and q_start stay as they are
+ * One call a layer's pages.  Errors: MP_EINVAL, MP_EHIP. */
+mp_status mp_paged_tree_plan(const mp_paged_kv* cache, const int32_t* parents, int32_t n_tokens, int32_t mask_words, uint64_t* mask,
+                             int32_t* positions, void* stream);
+mp_status mp_paged_tree_attention(const mp_paged_kv* cache, const void* q, int64_t q_stride, const uint64_t* mask, int32_t mask_words,
+                                  int32_t n_tokens, int32_t n_q_heads, int32_t max_new, int32_t window, float softmax_scale, void* out,
+                                  float* lse, void* workspace, size_t workspace_bytes, void* stream);
+mp_status mp_paged_tree_keep(const mp_paged_kv* cache, const uint64_t* mask, int32_t mask_words, int32_t n_tokens, const int32_t* leaf,
+                             int32_t* keep, void* stream);
 
 /* Library version string. */
 const char* mp_version(void);

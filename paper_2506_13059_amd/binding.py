@@ -23,7 +23,8 @@ EXPORTS = [
     "mp_get_centroids", "mp_get_selection", "mp_get_counters", "mp_get_layout", "mp_dense_workspace_bytes",
     "mp_dense_attention", "mp_version", "mp_enable_stage_timing", "mp_get_stage_timing", "mp_update_seed_counts", "mp_local_buffer_init", "mp_local_buffer_size", "mp_decode_step",
     "mp_dense_static_scratch_bytes", "mp_dense_attention_static", "mp_get_kv_codes", "mp_rotary_frequencies", "mp_rotary",
-    "mp_paged_append", "mp_paged_attention", "mp_paged_gather", "mp_paged_workspace_bytes",
+    "mp_paged_append", "mp_paged_attention", "mp_paged_gather", "mp_paged_workspace_bytes", "mp_norm_rotary", "mp_paged_append_norm", "mp_paged_reserve",
+    "mp_paged_tree_plan", "mp_paged_tree_attention", "mp_paged_tree_keep",
 ]
 
 MP_KV_BF16, MP_KV_E4M3 = 0, 1
@@ -45,6 +46,15 @@ class MpConfig(C.Structure):
 
 class MpRotarySpec(C.Structure):
     _fields_ = [("freqs", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float)]
+
+
+class MpHeadNormSpec(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("n_heads", C.c_int32), ("offset", C.c_float), ("eps", C.c_float)]
+
+
+class MpPagePoolArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("page_table", "kv_len", "q_start", "free_pages", "n_free")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_seqs", "table_stride")]
 
 
 class MpPagedKvArgs(C.Structure):
@@ -104,6 +114,12 @@ def lib():
         L.mp_paged_append.argtypes = [vp, vp, vp, i64, i32, vp, vp, i64, vp, i64, i32, vp]
         L.mp_paged_attention.argtypes = [vp, vp, i64, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp]
         L.mp_paged_gather.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp]
+        L.mp_norm_rotary.argtypes = [vp, vp, vp, i64, vp, i32, i32, vp, i64, vp, i32, vp]
+        L.mp_paged_append_norm.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, vp, vp, i64, vp, i64, i32, vp]
+        L.mp_paged_reserve.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp]
+        L.mp_paged_tree_plan.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+        L.mp_paged_tree_attention.argtypes = [vp, vp, i64, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.mp_paged_tree_keep.argtypes = [vp, vp, i32, i32, vp, vp, vp]
         L.mp_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
         L.mp_paged_workspace_bytes.restype = sz
         _lib = L
@@ -217,6 +233,22 @@ def mp_rotary_frequencies(rot_dim=128, base=10000.0, scaling=MP_ROTARY_PLAIN, fa
     return out
 
 
+class MpHeadNorm:
+    """Norm of a head's rows, x / sqrt(mean(x^2) + eps) * (weight + offset): weight bf16 [128], the same for all heads, or [heads, 128], on the current device."""
+
+    def __init__(self, weight, offset=0.0, eps=1e-6):
+        heads = weight.shape[0] if weight.dim() == 2 else 1
+        self.weight = _dense(weight, "weight", torch.bfloat16, (heads, 128) if weight.dim() == 2 else (128,), _here())
+        self.device = self.weight.get_device()
+        self.spec = MpHeadNormSpec(self.weight.data_ptr(), heads, offset, eps)
+        self.at = C.addressof(self.spec)
+
+    def _on(self, device):
+        if self.device != device:
+            _reject(f"the weights lie on device {self.device}, the tensors on device {device}")
+        return self.at
+
+
 class MpRotary:
     """Rotary positions: frequencies on the current device (given, or worked out by mp_rotary_frequencies), layout and amplitude."""
 
@@ -237,6 +269,13 @@ class MpRotary:
     def mp_rotary(self, x, positions=None, out=None, lookup_position=None, out_lookup=None):
         """x bf16 [tokens, heads, 128] at positions int32 [tokens] -> out (like x, densely packed; `out` may be x).  With a lookup_position:
         (out, out_lookup), out_lookup turned to that one position; positions may then be None for the second alone."""
+        return self._turn(None, x, positions, out, lookup_position, out_lookup)
+
+    def mp_norm_rotary(self, norm, x, positions=None, out=None, lookup_position=None, out_lookup=None):
+        """mp_rotary of rows that are normed first (norm: MpHeadNorm), in the same pass."""
+        return self._turn(norm, x, positions, out, lookup_position, out_lookup)
+
+    def _turn(self, norm, x, positions, out, lookup_position, out_lookup):
         device = _here()
         n, h, stride = _token_rows(x, "x", device)
         to_stride = to = look = at = 0
@@ -259,7 +298,8 @@ class MpRotary:
             look = out_lookup.data_ptr()
         elif out_lookup is not None:
             _reject("out_lookup needs a lookup_position")
-        st = lib().mp_rotary(self._on(device), x.data_ptr(), stride, at, n, h, to, to_stride, look, lookup_position or 0, _stream_of(device))
+        args = (self._on(device), x.data_ptr(), stride, at, n, h, to, to_stride, look, lookup_position or 0, _stream_of(device))
+        st = lib().mp_rotary(*args) if norm is None else lib().mp_norm_rotary(norm._on(device), *args)
         if st:
             _check(st)
         return out if lookup_position is None else (out, out_lookup)
@@ -296,6 +336,14 @@ class MpPagedKv:
 
     def mp_paged_append(self, k, v, rotary=None, q=None, q_out=None):
         """k, v bf16 [tokens, Hkv, 128] join the cache; returns the turned queries q_out [tokens, Hq, 128], or None without q."""
+        return self._append(k, v, rotary, q, q_out, False)
+
+    def mp_paged_append_norm(self, k, v, rotary=None, q=None, q_out=None, q_norm=None, k_norm=None, positions=None):
+        """mp_paged_append of queries and keys that are normed first (q_norm, k_norm: MpHeadNorm, or None for rows that are not), turned to positions int32
+        [tokens], or None: to where they stand in their sequences."""
+        return self._append(k, v, rotary, q, q_out, True, q_norm, k_norm, positions)
+
+    def _append(self, k, v, rotary, q, q_out, norms, q_norm=None, k_norm=None, positions=None):
         device = self._current()
         n, h, ks = _token_rows(k, "k", device)
         nv, hv, vs = _token_rows(v, "v", device)
@@ -313,8 +361,13 @@ class MpPagedKv:
             from_, to = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             _reject("q_out needs q")
-        st = lib().mp_paged_append(self.at, None if rotary is None else rotary._on(device), from_, qs, hq, to, k.data_ptr(), ks, v.data_ptr(), vs, n,
-                                   _stream_of(device))
+        turn = None if rotary is None else rotary._on(device)
+        rows = (from_, qs, hq, to, k.data_ptr(), ks, v.data_ptr(), vs, n, _stream_of(device))
+        if norms:
+            at = 0 if positions is None else _dense(positions, "positions", torch.int32, (n,), device).data_ptr()
+            st = lib().mp_paged_append_norm(self.at, turn, None if q_norm is None else q_norm._on(device), None if k_norm is None else k_norm._on(device), at, *rows)
+        else:
+            st = lib().mp_paged_append(self.at, turn, *rows)
         if st:
             _check(st)
         return q_out
@@ -323,6 +376,13 @@ class MpPagedKv:
         """q bf16 [tokens, Hq, 128] -> out bf16 [tokens, Hq, 128] (and lse fp32 [tokens, Hq]); max_new: as many new tokens a sequence at most.  0 stands for
         as many as q has: a decode step passes 1, which takes the kernel for it, probabilities in two bf16 parts and 4 MiB of workspace.  Without a workspace one is
         allocated (up to 69 MiB)."""
+        return self._attend(q, None, max_new, window, softmax_scale, out, lse, workspace)
+
+    def mp_paged_tree_attention(self, q, mask, max_new=0, window=0, softmax_scale=0.0, out=None, lse=None, workspace=None):
+        """mp_paged_attention of a tree's tokens: each attends its sequence's older keys and the new ones that its mask (int64 [tokens, words]) marks."""
+        return self._attend(q, mask, max_new, window, softmax_scale, out, lse, workspace)
+
+    def _attend(self, q, mask, max_new, window, softmax_scale, out, lse, workspace):
         device = self._current()
         n, hq, qs = _token_rows(q, "q", device)
         if out is None:
@@ -335,11 +395,46 @@ class MpPagedKv:
             workspace = torch.empty(mp_paged_workspace_bytes(n, hq, self.n_kv_heads, self.n_seqs, max_new), dtype=torch.uint8, device=q.device)
         elif workspace.get_device() != device or not workspace.is_contiguous():
             _reject(f"workspace: a contiguous tensor on the current device expected, got one on {workspace.device}")
-        st = lib().mp_paged_attention(self.at, q.data_ptr(), qs, n, hq, max_new, window, softmax_scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                      workspace.data_ptr(), workspace.nbytes, _stream_of(device))
+        rest = (n, hq, max_new, window, softmax_scale, out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_of(device))
+        if mask is None:
+            st = lib().mp_paged_attention(self.at, q.data_ptr(), qs, *rest)
+        else:
+            at, words = self._mask(mask, n, device)
+            st = lib().mp_paged_tree_attention(self.at, q.data_ptr(), qs, at, words, *rest)
         if st:
             _check(st)
         return out
+
+    def _mask(self, mask, n, device):
+        if mask.dim() != 2:
+            _reject(f"mask: int64 [{n}, words] expected, got {tuple(mask.shape)}")
+        return _dense(mask, "mask", torch.int64, (n, mask.shape[1]), device).data_ptr(), mask.shape[1]
+
+    def mp_paged_tree_plan(self, parents, mask_words=1, mask=None, positions=None):
+        """parents int32 [tokens], numbers within a sequence's new tokens (no token before it: none) -> (mask int64 [tokens, mask_words] of each token and its
+        ancestors, positions int32 [tokens]).  Rows of no sequence are left as they were: where that matters, pass tensors."""
+        device = self._current()
+        n = parents.shape[0] if parents.dim() == 1 else -1
+        _dense(parents, "parents", torch.int32, (n,), device)
+        mask = parents.new_empty((n, mask_words), dtype=torch.int64) if mask is None else _dense(mask, "mask", torch.int64, (n, mask_words), device)
+        positions = parents.new_empty((n,)) if positions is None else _dense(positions, "positions", torch.int32, (n,), device)
+        st = lib().mp_paged_tree_plan(self.at, parents.data_ptr(), n, mask_words, mask.data_ptr(), positions.data_ptr(), _stream_of(device))
+        if st:
+            _check(st)
+        return mask, positions
+
+    def mp_paged_tree_keep(self, mask, leaf, keep=None):
+        """The rows of the path that ends in new token leaf[b] (int32 [n_seqs]; anything else: none) moved together behind the older ones -> keep int32 [n_seqs], the
+        keys that stay of each sequence."""
+        device = self._current()
+        n = mask.shape[0]
+        at, words = self._mask(mask, n, device)
+        _dense(leaf, "leaf", torch.int32, (self.n_seqs,), device)
+        keep = leaf.new_empty((self.n_seqs,)) if keep is None else _dense(keep, "keep", torch.int32, (self.n_seqs,), device)
+        st = lib().mp_paged_tree_keep(self.at, at, words, n, leaf.data_ptr(), keep.data_ptr(), _stream_of(device))
+        if st:
+            _check(st)
+        return keep
 
     def mp_paged_gather(self, n, first=0, rotary=None, lookup_position=None, k=None, v=None, k_lookup=None):
         """Keys and values [first, first + n) of every sequence: (k, v) bf16 [n_seqs, Hkv, n, 128], with a lookup_position (k, v, k_lookup).  Rows that a
@@ -361,6 +456,46 @@ class MpPagedKv:
             _check(lib().mp_paged_gather(self.at, None if rotary is None else rotary._on(device), first, n, lookup_position or 0, k.data_ptr(), look, v.data_ptr(),
                                          _stream_of(device)))
         return (k, v) if lookup_position is None else (k, v, k_lookup)
+
+
+class MpPagePool:
+    """Pages in no use beside the tensors of an MpPagedKv (the same page_table, kv_len and q_start): free_pages int32 [n_pages], a stack of which the first n_free
+    (int32 [1]) entries count.  The tensors are kept, not copied, and changed in place."""
+
+    def __init__(self, page_table, kv_len, q_start, free_pages, n_free, page_size):
+        device = self.device = _here()
+        if page_table.dim() != 2 or free_pages.dim() != 1:
+            _reject(f"page_table [n_seqs, pages] and free_pages [n_pages] expected, got {tuple(page_table.shape)} and {tuple(free_pages.shape)}")
+        self.n_seqs, columns = page_table.shape
+        _dense(page_table, "page_table", torch.int32, page_table.shape, device)
+        _dense(kv_len, "kv_len", torch.int32, (self.n_seqs,), device)
+        _dense(q_start, "q_start", torch.int32, (self.n_seqs + 1,), device)
+        _dense(free_pages, "free_pages", torch.int32, free_pages.shape, device)
+        _dense(n_free, "n_free", torch.int32, (1,), device)
+        self.tensors = (page_table, kv_len, q_start, free_pages, n_free)
+        self.args = MpPagePoolArgs(*(t.data_ptr() for t in self.tensors), free_pages.shape[0], page_size, self.n_seqs, columns)
+        self.at = C.addressof(self.args)
+
+    def mp_paged_reserve(self, n_new, keep=None, granted=None, sequence=None, positions=None, slots=None):
+        """Pages of keys past keep (int32 [n_seqs]; None: all stay) go back, n_new (int32 [n_seqs]) tokens get theirs; kv_len and q_start follow.  granted int32 [n_seqs],
+        and of the step's rows sequence, positions int32 [rows], slots int64 [rows] are written where they are passed (as many rows in each)."""
+        device = _here()
+        if self.device != device:
+            _reject(f"the pool lies on device {self.device}, not on the current device {device}")
+        _dense(n_new, "n_new", torch.int32, (self.n_seqs,), device)
+        if keep is not None:
+            _dense(keep, "keep", torch.int32, (self.n_seqs,), device)
+        if granted is not None:
+            _dense(granted, "granted", torch.int32, (self.n_seqs,), device)
+        rows = None
+        for t, name, dtype in ((sequence, "sequence", torch.int32), (positions, "positions", torch.int32), (slots, "slots", torch.int64)):
+            if t is not None:
+                rows = (t.shape[0] if t.dim() == 1 else -1) if rows is None else rows
+                _dense(t, name, dtype, (rows,), device)
+        st = lib().mp_paged_reserve(self.at, n_new.data_ptr(), *(None if t is None else t.data_ptr() for t in (keep, granted, sequence, positions, slots)), rows or 0,
+                                    _stream_of(device))
+        if st:
+            _check(st)
 
 
 class MpContext:

@@ -3,7 +3,7 @@
 // Query row i of a sequence with n new tokens and len keys (the new ones among them) stands at position p = len - n + i and attends the
 // keys j with p - window < j <= p (window 0: all up to p) whose page is there:
 //     o = sum_j e^(s q.k_j - m) v_j / l,   l = sum_j e^(s q.k_j - m),   lse = m + ln l,
-// a row without such a key gives zeros and -inf.
+// a row without such a key gives zeros and -inf.  A token of a tree attends the keys j < len - n and those of the new ones that its mask marks, the last `window` of them all.
 #include "mp_paged.h"
 
 namespace mp {
@@ -48,15 +48,23 @@ size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_s
 }
 
 // A head's blocks on the line (mp_paged_plan.h) at most, in the kernel that has the smaller tiles, blocks and more places in front; tiles: what all tokens fill, and one that is not full a sequence.
-bool paged_line_fits(const PagedAttention& a)
+// `span`: new tokens whose keys a tile's rows may attend.
+static bool line_fits(const PagedAttention& a, long long tokens, long long span)
 {
-    const long long tokens = 256 / (a.n_q_heads / a.c.n_kv), room = (long long)a.c.table_stride << a.c.page_shift;
-    const long long keys = a.window > 0 && a.window + tokens < room ? a.window + tokens : room;
+    const long long room = (long long)a.c.table_stride << a.c.page_shift;
+    const long long keys = a.window > 0 && a.window + span < room ? a.window + span : room;
     const long long tiles = a.n_tokens / tokens + (a.c.n_seqs < a.n_tokens ? a.c.n_seqs : a.n_tokens);
     return tiles * (keys / 64 + 5) < 1ll << 32;
 }
+bool paged_line_fits(const PagedAttention& a)
+{
+    const long long tokens = 256 / (a.n_q_heads / a.c.n_kv);
+    return line_fits(a, tokens, tokens);
+}
+bool paged_line_fits(const PagedTreeAttention& a) { return line_fits(a, 256 / (a.n_q_heads / a.c.n_kv), a.max_new); }
 
-hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s)
+template <class A>
+static hipError_t launch_attention(const A& a, hipStream_t s)
 {
     if (a.n_tokens <= 0 || a.c.n_seqs <= 0) return hipSuccess;
     Kernels k = kernels_of(a.n_tokens, a.n_q_heads / a.c.n_kv, a.c.n_seqs, a.max_new);
@@ -69,5 +77,7 @@ hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s)
     }
     return k.chunks ? launch_paged_chunks(a, k.tokens, room, s) : hipSuccess;
 }
+hipError_t launch_paged_attention(const PagedAttention& a, hipStream_t s) { return launch_attention(a, s); }
+hipError_t launch_paged_attention(const PagedTreeAttention& a, hipStream_t s) { return launch_attention(a, s); }
 
 }  // namespace mp

@@ -10,6 +10,8 @@
 // 175 instructions a block and wave) 46 %, both as counted.  Eight waves, so that each SIMD has two: one computes where the other waits.  What brought it there, the same call: rows
 // through registers, one block ahead 5.03 ms; straight to LDS 4.73; loads among the products 4.46; cheaper shares and page entries 4.35; waves that meet every second block 4.31; maxima 4.20 -> 4.12.
 // Did nothing: waves of a SIMD half a block apart, priorities, more reads ahead.
+#include <type_traits>
+
 #include "mp_paged_plan.h"
 
 namespace mp {
@@ -111,9 +113,6 @@ __device__ __forceinline__ unsigned long long lds_read8(uint32_t at)        // t
 // (not waited for: the wave's next read is)
 __device__ __forceinline__ void lds_write1(uint32_t at, uint32_t v) { asm volatile("ds_write_b8 %0, %1" ::"v"(at), "v"(v) : "memory"); }
 
-// The lowest n of 64 bits.
-__device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
-
 // (a denominator of 0: no key, or none of any weight; NaN, of a logit that is NaN or +inf, stays)
 __device__ __forceinline__ float lse_of(float m, float l) { return l != 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY; }
 
@@ -163,10 +162,20 @@ __device__ __forceinline__ void store_part(float* part, const Softmax& st, float
     }
 }
 
-// kOnePage: pages of eight rows or more.  (Smaller ones take addresses a lane, and eight registers more than there are: 2048 tokens at 32K 1.06 ms for 1.02.)
-template <bool kOnePage>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
+// Which keys of a block a row of a tree attends (see TreeRow), `base` of them older than the new ones: a bit for each.
+__device__ __forceinline__ unsigned long long tree_keys(const TreeRow& row, int words, int base, int block)
 {
+    const int at = block * kKeys - base, w = at >> 6, by = at & 63;      // of the block's first key among the new ones
+    unsigned long long marked = w >= 0 && w < words ? row.mask[w] >> by : 0ull;
+    if (by && w + 1 >= 0 && w + 1 < words) marked |= row.mask[w + 1] << (64 - by);
+    return (below(-at) | marked) & ~below(row.low - block * kKeys);
+}
+
+// kOnePage: pages of eight rows or more.  (Smaller ones take addresses a lane, and eight registers more than there are: 2048 tokens at 32K 1.06 ms for 1.02.)
+template <bool kOnePage, class A>
+__device__ __forceinline__ void attend(const A& a, const Tiling& tl, float* parts, Cut* cuts)
+{
+    constexpr bool kTree = std::is_same<A, PagedTreeAttention>::value;
     __shared__ __align__(256) unsigned char lds[kRing * kBlockBytes + 2 * kRing * kWaves];
     const uint32_t ring = lds_offset(lds), valid_at = ring + kRing * kBlockBytes, odd_at = valid_at + kRing * kWaves;      // (a byte a wave: keys that are there; whose values are not all finite)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
@@ -211,6 +220,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const int position = it.rows.base + i;
         const bool active = wave * 32 < tile_rows;
         const int pos_min = lane_value(position, 0), pos_max = lane_value(position, 31);
+        TreeRow row{};
+        int words = 0;
+        if constexpr (kTree) {
+            row = tree_row(a, it.rows, i);
+            words = min(a.words, (it.rows.n + 63) >> 6);
+        }
         bf16x8 q[8];
         {
             const uint4* from = reinterpret_cast<const uint4*>(a.q + (long long)(it.rows.q0 + i) * a.q_stride + (long long)head * kHeadDim);
@@ -278,7 +293,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         };
         // Blocks in which some row of the item sees a key that another one does not: those from edge_from on, and with a window those up to edge_upto.
         const int low = it.rows.base + it.tile * tl.tokens, high = it.rows.base + min(it.rows.n, (it.tile + 1) * tl.tokens) - 1;
-        const int edge_from = low < 0 ? -1 : (low + 1) / kKeys, edge_upto = a.window && high >= a.window ? (high - a.window) / kKeys : -1;
+        int edge_from = low < 0 ? -1 : (low + 1) / kKeys, edge_upto = a.window && high >= a.window ? (high - a.window) / kKeys : -1;
+        if constexpr (kTree) {
+            const TreeEdges e = tree_edges(a, it.rows);
+            edge_from = e.from / kKeys;
+            edge_upto = e.upto > 0 ? (e.upto - 1) / kKeys : -1;
+        }
         auto edge = [&](int block) { return block >= edge_from || block <= edge_upto; };
         // When the wave's rows of a block have come: values of rows that are not there are zeroed (a probability of zero meets them), and so are those of an
         // edge's block that are not finite, lest they meet the zero of a row that does not see them.
@@ -349,7 +369,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 block = min(t + 3, last - 1);
                 entry = entry_at(block);
                 // (with this as the `else` of what follows, its state was copied at the end of both, and registers ran out)
-                const bool sees_some = active && t * kKeys <= pos_max;
+                const bool sees_some = active && (kTree || t * kKeys <= pos_max);
                 if (!sees_some) load_all(coming);
                 if (sees_some) {
                 // (keys and values are read a half at a time: with all of a block's keys at once, registers run out)
@@ -374,11 +394,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 s16x4 v[16];
                 read_values(v, v_at, slot);
                 const unsigned long long valid = lds_read8(valid_at + (uint32_t)((t & (kRing - 1)) * kWaves));
-                const bool masked = valid != ~0ull || t * kKeys + kKeys - 1 > pos_min || (a.window && t * kKeys <= pos_max - a.window);
+                const bool masked = valid != ~0ull || (kTree ? edge(t) : t * kKeys + kKeys - 1 > pos_min || (a.window && t * kKeys <= pos_max - a.window));
                 if (masked) {
                     // keys (from, upto] of the block, those that are there; bit k of `see` for key 4 half + k
-                    const int upto = position - t * kKeys, from = a.window ? upto - a.window : -1;
-                    const unsigned long long see = (valid & below(upto + 1) & ~below(from + 1)) >> (4 * half);
+                    unsigned long long keys;
+                    if constexpr (kTree) {
+                        keys = tree_keys(row, words, it.rows.base, t);
+                    } else {
+                        const int upto = position - t * kKeys, from = a.window ? upto - a.window : -1;
+                        keys = below(upto + 1) & ~below(from + 1);
+                    }
+                    const unsigned long long see = (valid & keys) >> (4 * half);
 #pragma unroll
                     for (int tt = 0; tt < 2; ++tt) {
                         const uint32_t in = (uint32_t)(see >> (32 * tt));
@@ -432,7 +458,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     for (unsigned long long odd = lds_read8(odd_at + (t & (kRing - 1)) * kWaves); odd; odd &= odd - 1) {
                         const int key = t * kKeys + __ffsll((long long)odd) - 1;
                         const int page = __builtin_amdgcn_readfirstlane(page_of(entries, a.c.table_stride, a.c.n_pages, a.c.page_shift, key));
-                        const bool sees = key <= position && !(a.window && key <= position - a.window);
+                        bool sees = key <= position && !(a.window && key <= position - a.window);
+                        if constexpr (kTree) sees = tree_keys(row, words, it.rows.base, t) >> (key & (kKeys - 1)) & 1;
                         const uint2* from = reinterpret_cast<const uint2*>(a.c.V + row_of(max(page, 0), h, a.c.n_kv, a.c.page_shift, key) * kHeadDim);
 #pragma unroll
                         for (int d = 0; d < 4; ++d)
@@ -465,6 +492,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         }
     }
     if (threadIdx.x == 0) cuts[share] = cut;
+}
+
+template <bool kOnePage>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_chunk_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
+{
+    attend<kOnePage>(a, tl, parts, cuts);
+}
+template <bool kOnePage>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tree_chunk_kernel(PagedTreeAttention a, Tiling tl, float* parts, Cut* cuts)
+{
+    attend<kOnePage>(a, tl, parts, cuts);
 }
 
 // One wave a cut, 32 rows and 32 dims.
@@ -505,21 +543,30 @@ __global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a,
 
 constexpr size_t kCutFloats = sizeof(Cut) / sizeof(float) * kWorkgroups;
 
-}  // namespace
+template <bool kOnePage>
+auto kernel_of(const PagedAttention&) { return paged_chunk_kernel<kOnePage>; }
+template <bool kOnePage>
+auto kernel_of(const PagedTreeAttention&) { return paged_tree_chunk_kernel<kOnePage>; }
 
-size_t paged_chunk_floats() { return (size_t)2 * kWorkgroups * kPartFloats + kCutFloats; }
-
-hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s)
+template <class A>
+hipError_t launch(const A& a, int over, float* room, hipStream_t s)
 {
     const Tiling tl = tiling(a.n_q_heads / a.c.n_kv, kRows, over, 0x7fffffff, kKeys, 3, 4);
     Cut* cuts = reinterpret_cast<Cut*>(room);
     float* parts = room + kCutFloats;
-    const auto kernel = a.c.page_shift >= 3 ? paged_chunk_kernel<true> : paged_chunk_kernel<false>;
+    const auto kernel = a.c.page_shift >= 3 ? kernel_of<true>(a) : kernel_of<false>(a);
     hipLaunchKernelGGL(kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(32 * kWorkgroups), dim3(64), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
+    hipLaunchKernelGGL(paged_chunk_merge_kernel, dim3(32 * kWorkgroups), dim3(64), 0, s, (const PagedAttention&)a, tl.group, (const float*)parts, (const Cut*)cuts);
     return hipGetLastError();
 }
+
+}  // namespace
+
+size_t paged_chunk_floats() { return (size_t)2 * kWorkgroups * kPartFloats + kCutFloats; }
+
+hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s) { return launch(a, over, room, s); }
+hipError_t launch_paged_chunks(const PagedTreeAttention& a, int over, float* room, hipStream_t s) { return launch(a, over, room, s); }
 
 }  // namespace mp

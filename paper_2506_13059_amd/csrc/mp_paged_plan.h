@@ -76,6 +76,50 @@ __device__ __forceinline__ void blocks_of_tile(const PagedAttention& a, const Ti
     const int i0 = tile * tl.tokens;
     blocks_of(r.base, i0, min(r.n, i0 + tl.tokens) - 1, a.window, room_of(a), tl.unit, b0, b1);
 }
+// (of a tree: from the older keys that a window leaves a token without marks, to the last new one, whichever the tile)
+__device__ __forceinline__ void blocks_of_tile(const PagedTreeAttention& a, const Tiling& tl, const SequenceRows& r, int, int* b0, int* b1)
+{
+    blocks_of(r.base - 1, 0, r.n, a.window, room_of(a), tl.unit, b0, b1);
+}
+
+// What a query row attends: keys that are older than the new ones, from the row's first on (one key behind another, the last of them and the row's marks fill the window), and marked ones.
+struct TreeRow {
+    const unsigned long long* mask;
+    int low;                  // first key; if it is no older one, marks before it do not count
+};
+__device__ __forceinline__ TreeRow tree_row(const PagedTreeAttention& a, const SequenceRows& r, int i)
+{
+    TreeRow t{a.mask + (long long)(r.q0 + i) * a.words, 0};
+    if (a.window > 0) {
+        int left = a.window;
+        t.low = -1;
+        for (int w = min(a.words, (r.n + 63) >> 6) - 1; w >= 0; --w) {
+            const int in = r.n - 64 * w;
+            unsigned long long m = t.mask[w];
+            if (in < 64) m &= (1ull << in) - 1ull;
+            const int n = __popcll(m);
+            if (n >= left) {
+                while (--left > 0) m &= ~(1ull << (63 - __clzll((long long)m)));
+                t.low = r.base + 64 * w + 63 - __clzll((long long)m);
+                break;
+            }
+            left -= n;
+        }
+        if (left > 0) t.low = max(r.base, left) - left;
+    }
+    return t;
+}
+// The lowest n of 64 bits.
+__device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
+// Keys of a sequence that are attended by all of its rows or by none lie before the first of these and behind the second, see edges.
+struct TreeEdges {
+    int upto, from;           // keys before `upto` are not seen by some rows (a window's), keys from `from` on may be new ones
+};
+__device__ __forceinline__ TreeEdges tree_edges(const PagedTreeAttention& a, const SequenceRows& r)
+{
+    return TreeEdges{a.window > 0 ? r.base - max(a.window - r.n, 0) : 0, max(r.base, 0)};
+}
+
 
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 __device__ __forceinline__ int tiles_of(const Tiling& tl, const SequenceRows& r)
@@ -98,8 +142,8 @@ __device__ __forceinline__ void take_item(Item* it, int at, int b, int tile, con
 
 // Returns the places of one head's items in all, `ahead` of them in front of each one's blocks (*items: how many there are); kFind: goes up to the item that
 // place x of the line lies in, puts it into *found and returns x (anything else: there is none).  One wave, 64 sequences (or, where some have several tiles, 64 tiles) at a time.  `head`: rows_of_lane(a, 0).
-template <bool kFind>
-__device__ __forceinline__ uint32_t walk(const PagedAttention& a, const Tiling& tl, const SequenceRows& head, int ahead, uint32_t x, Item* found, uint32_t* items)
+template <bool kFind, class A>
+__device__ __forceinline__ uint32_t walk(const A& a, const Tiling& tl, const SequenceRows& head, int ahead, uint32_t x, Item* found, uint32_t* items)
 {
     const int lane = threadIdx.x & 63;
     uint32_t sum = 0;
@@ -160,7 +204,8 @@ __device__ __forceinline__ long long quotient(long long x, long long d)
     return ((x | d) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;
 }
 // Looks at sequences s0 .., whose rows are in l->head.
-__device__ __forceinline__ void look_at(const PagedAttention& a, const Tiling& tl, Line* l, int s0, uint32_t before)
+template <class A>
+__device__ __forceinline__ void look_at(const A& a, const Tiling& tl, Line* l, int s0, uint32_t before)
 {
     const bool there = tiles_of(tl, l->head) > 0;
     l->s0 = s0;
@@ -171,8 +216,8 @@ __device__ __forceinline__ void look_at(const PagedAttention& a, const Tiling& t
     l->total = (uint32_t)lane_value((int)l->incl, 63);
 }
 // kSingle: no sequence of the tiling has more than one tile.
-template <bool kSingle>
-__device__ __forceinline__ Line line_of(const PagedAttention& a, const Tiling& tl)
+template <bool kSingle, class A>
+__device__ __forceinline__ Line line_of(const A& a, const Tiling& tl)
 {
     Line l;
     l.head = rows_of_lane(a, 0);
@@ -223,8 +268,8 @@ __device__ __forceinline__ long long blocks_from(const Item& it, const Line& lin
     return (long long)h * line.of_head + it.before + line.ahead;
 }
 // `known`: s->it is the item before, which ended at x.
-template <bool kSingle>
-__device__ __forceinline__ void segment_at(const PagedAttention& a, const Tiling& tl, Line& line, long long x, long long end, bool known, Segment* s)
+template <bool kSingle, class A>
+__device__ __forceinline__ void segment_at(const A& a, const Tiling& tl, Line& line, long long x, long long end, bool known, Segment* s)
 {
     Item& it = s->it;
     bool found = true;

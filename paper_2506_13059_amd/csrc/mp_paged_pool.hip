@@ -1,0 +1,235 @@
+// Page tables, and the maps of a step's tokens, made on the device from what sequences keep and what is to come, for gfx950.
+//
+// Of sequence b with `have` keys, of which stay = min(keep, have) are kept, entries [ceil(stay / P), ceil(have / P)) of its table are given back: their pages go on the
+// stack of free ones, sequence after sequence, entry after entry.  Then each sequence takes ceil((stay + new) / P) - ceil(stay / P) pages from the top of the stack, sequence after
+// sequence; the first that finds too few gets no tokens, and neither does any behind it that needs pages.
+//
+// One workgroup, for everything hangs on two running sums over the sequences: bound by its trips to memory one behind the other.  The maps of many tokens are a launch of their own.
+#include "mp_device.h"
+#include "mp_paged.h"
+
+namespace mp {
+
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kDeep = 8;
+
+struct Shared {
+    uint32_t upto[kThreads];            // of a flat list of sequences' entries: where each one's end
+    int32_t left[kThreads];             // first entry
+    uint32_t sums[2][kWaves];
+    uint32_t counts[2][kDeep * kWaves];
+    unsigned long long tokens[kWaves];
+    uint32_t taken;
+};
+
+// Inclusive sum over the workgroup; *all: the sum of everything.  `which`: the two buffers in turn.
+__device__ __forceinline__ uint32_t block_scan(Shared& sm, int which, uint32_t v, uint32_t* all)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const uint32_t incl = wave_incl_scan_u32(v);
+    if (lane == 63) sm.sums[which][wave] = incl;
+    __syncthreads();
+    uint32_t before = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const uint32_t s = sm.sums[which][w];
+        before += w < wave ? s : 0u;
+        sum += s;
+    }
+    *all = sum;
+    return before + incl;
+}
+
+// The first of the sequences whose entries end behind place x of the list.
+__device__ __forceinline__ int owner_of(const Shared& sm, uint32_t x)
+{
+    int k = 0;
+#pragma unroll
+    for (int step = kThreads / 2; step; step >>= 1)
+        if (sm.upto[k + step - 1] <= x) k += step;
+    return k;
+}
+
+struct Sequence {
+    int have, stay, left, had;           // keys, keys that stay, and their pages
+};
+__device__ __forceinline__ Sequence sequence_at(const PagePool& p, const int32_t* keep, int b)
+{
+    Sequence s{0, 0, 0, 0};
+    if (b < p.n_seqs) {
+        const int room = p.table_stride << p.page_shift, len = p.kv_len[b];
+        s.have = min(max(len, 0), room);
+        s.stay = min(max(keep ? keep[b] : len, 0), s.have);
+        const uint32_t up = (1u << p.page_shift) - 1u;
+        s.left = (int)(((uint32_t)s.stay + up) >> p.page_shift);
+        s.had = (int)(((uint32_t)s.have + up) >> p.page_shift);
+    }
+    return s;
+}
+
+// Rows r0 + lane of a step: their sequence, position and place in the cache.
+__device__ __forceinline__ void map_rows(const PagePool& p, const StepRows& rows, int r0)
+{
+    const int lane = threadIdx.x & 63, r = r0 + lane;
+    const int first = sequence_of(p.q_start, p.n_seqs, r0);
+    int b = first >= 0 ? first : p.n_seqs;
+    for (int s = first + 1; first >= 0;  s += 64) {
+        const int start = s + lane <= p.n_seqs ? p.q_start[s + lane] : 0x7fffffff;
+        int k = 0;                                          // how many of these starts lie at or before r
+#pragma unroll
+        for (int step = 32; step; step >>= 1)
+            if (__shfl(start, k + step - 1, 64) <= r) k += step;
+        if (__shfl(start, k, 64) <= r) ++k;                 // (63 of them: perhaps all)
+        if (k > 0) b = s - 1 + k;
+        if (!__any(k == 64)) break;
+    }
+    if (r >= rows.n_rows) return;
+    int position = -1;
+    long long slot = -1;
+    if (b < p.n_seqs) {
+        position = p.kv_len[b] - (p.q_start[b + 1] - r);
+        if (rows.slots) {
+            const int page = page_of(p.table + (long long)b * p.table_stride, p.table_stride, p.n_pages, p.page_shift, position);
+            if (page >= 0) slot = ((long long)page << p.page_shift) + (position & ((1 << p.page_shift) - 1));
+        }
+    }
+    if (rows.sequence) rows.sequence[r] = b < p.n_seqs ? b : -1;
+    if (rows.positions) rows.positions[r] = position;
+    if (rows.slots) rows.slots[r] = slot;
+}
+
+__global__ __launch_bounds__(kThreads) void paged_reserve_kernel(PagePool p, const int32_t* n_new, const int32_t* keep, int32_t* granted, StepRows rows)
+{
+    __shared__ Shared sm;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    int32_t* const stack = p.free_pages;
+    uint32_t top = (uint32_t)min(max(p.n_free[0], 0), p.n_pages);
+    Sequence seq{};
+    // Pages that go back.
+    int turn = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
+        seq = sequence_at(p, keep, s0 + tid);
+        uint32_t all;
+        const uint32_t incl = block_scan(sm, 0, (uint32_t)(seq.had - seq.left), &all);
+        sm.upto[tid] = incl;
+        sm.left[tid] = seq.left;
+        __syncthreads();
+        for (uint32_t x0 = 0; x0 < all; x0 += kDeep * kThreads, turn ^= 1) {
+            int32_t page[kDeep];
+            unsigned long long in[kDeep];
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const uint32_t x = x0 + (uint32_t)(i * kThreads + tid);
+                page[i] = -1;
+                if (x < all) {
+                    const int k = owner_of(sm, x);
+                    int32_t* const entry = p.table + (long long)(s0 + k) * p.table_stride + sm.left[k] + (int)(x - (k ? sm.upto[k - 1] : 0u));
+                    page[i] = *entry;
+                    *entry = -1;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                in[i] = __ballot((uint32_t)page[i] < (uint32_t)p.n_pages);
+                if (lane == 0) sm.counts[turn][i * kWaves + wave] = (uint32_t)__popcll(in[i]);
+            }
+            __syncthreads();
+            const uint32_t c0 = sm.counts[turn][2 * lane], c1 = sm.counts[turn][2 * lane + 1];
+            const uint32_t upto = wave_incl_scan_u32(c0 + c1);
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const int at = i * kWaves + wave;
+                uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(upto - c0 - c1), at >> 1);
+                if (at & 1) before += (uint32_t)__builtin_amdgcn_readlane((int)c0, at >> 1);
+                const uint32_t to = top + before + (uint32_t)__popcll(in[i] & ((1ull << lane) - 1ull));
+                if ((in[i] >> lane & 1) && to < (uint32_t)p.n_pages) stack[to] = page[i];      // (more than there are: a page that came twice)
+            }
+            top += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        }
+        __syncthreads();
+    }
+    top = min(top, (uint32_t)p.n_pages);
+    // Pages for the tokens to come.
+    uint32_t needed = 0, taken = 0;
+    unsigned long long tokens = 0;
+    if (tid == 0) p.q_start[0] = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
+        const int b = s0 + tid;
+        if (p.n_seqs > kThreads) seq = sequence_at(p, keep, b);
+        const int room = p.table_stride << p.page_shift;
+        int come = b < p.n_seqs ? max(n_new[b], 0) : 0;
+        if (come > room - seq.stay) come = 0;
+        const uint32_t need = ((uint32_t)(seq.stay + come) + ((1u << p.page_shift) - 1u)) >> p.page_shift;
+        const uint32_t more = come > 0 ? need - (uint32_t)seq.left : 0u;
+        uint32_t all;
+        const uint32_t incl = block_scan(sm, 1, more, &all);
+        const bool ok = more == 0 || needed + incl <= top;
+        if (!ok) come = 0;
+        sm.upto[tid] = incl;
+        sm.left[tid] = seq.left;
+        if (tid == 0) sm.taken = 0;
+        // tokens up to each one's
+        unsigned long long upto = (unsigned long long)come;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) {
+            const unsigned long long v = __shfl_up(upto, step, 64);
+            if (lane >= step) upto += v;
+        }
+        if (lane == 63) sm.tokens[wave] = upto;
+        __syncthreads();
+        if (ok && more > 0) atomicMax(&sm.taken, incl);
+        unsigned long long sum = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) upto += sm.tokens[w];
+            sum += sm.tokens[w];
+        }
+        if (b < p.n_seqs) {
+            p.kv_len[b] = seq.stay + come;
+            p.q_start[b + 1] = (int32_t)min(tokens + upto, 0x7fffffffull);
+            if (granted) granted[b] = come;
+        }
+        tokens += sum;
+        __syncthreads();
+        const uint32_t here = sm.taken;
+        for (uint32_t x = tid; x < here; x += kThreads) {
+            const int k = owner_of(sm, x);
+            int32_t* const from = stack + (top - 1u - (taken + x));
+            p.table[(long long)(s0 + k) * p.table_stride + sm.left[k] + (int)(x - (k ? sm.upto[k - 1] : 0u))] = *from;
+            *from = -1;
+        }
+        taken += here;
+        needed += all;
+        __syncthreads();
+    }
+    if (tid == 0) p.n_free[0] = (int32_t)(top - taken);
+    if (rows.n_rows > 0) {
+        __syncthreads();
+        for (int r0 = wave * 64; r0 < rows.n_rows; r0 += kThreads) map_rows(p, rows, r0);
+    }
+}
+
+__global__ __launch_bounds__(256) void paged_map_kernel(PagePool p, StepRows rows)
+{
+    const int r0 = blockIdx.x * 256 + (threadIdx.x & ~63);
+    if (r0 < rows.n_rows) map_rows(p, rows, r0);
+}
+
+constexpr int kMapped = 4096;            // rows that the one workgroup maps itself
+
+}  // namespace
+
+hipError_t launch_paged_reserve(const PagePool& p, const int32_t* n_new, const int32_t* keep, int32_t* granted, const StepRows& rows, hipStream_t s)
+{
+    const bool apart = rows.n_rows > kMapped;
+    StepRows here = rows;
+    if (apart) here.n_rows = 0;
+    hipLaunchKernelGGL(paged_reserve_kernel, dim3(1), dim3(kThreads), 0, s, p, n_new, keep, granted, here);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !apart) return e;
+    hipLaunchKernelGGL(paged_map_kernel, dim3((unsigned)(((long long)rows.n_rows + 255) / 256)), dim3(256), 0, s, p, rows);
+    return hipGetLastError();
+}
+
+}  // namespace mp

@@ -54,11 +54,69 @@ struct Source {
     int stride, n_pages, shift, n_kv, h, end;
 };
 
+// Which keys the lane's query rows attend.  edge: some row of the tile sees one of its keys that another one does not.
+template <int kGroups, class A>
+struct Seen;
+template <int kGroups>
+struct Seen<kGroups, PagedAttention> {       // those up to their own position, the last `window` of them
+    int position[kGroups], pos_min, pos_max, window;
+    __device__ __forceinline__ void item(const PagedAttention& a, const Item& it, int first, int tokens)
+    {
+        pos_min = it.rows.base + first;
+        pos_max = pos_min + tokens - 1;
+        window = a.window;
+    }
+    __device__ __forceinline__ void row(const PagedAttention&, const Item& it, int r, int i) { position[r] = it.rows.base + i; }
+    __device__ __forceinline__ int end() const { return pos_max + 1; }
+    __device__ __forceinline__ bool edge(int t) const { return t * kTile + kTile - 1 > pos_min || (window && t * kTile <= pos_max - window); }
+    struct Tile {
+        int upto, from;
+        __device__ __forceinline__ bool operator()(int key) const { return key <= upto && key > from; }
+    };
+    __device__ __forceinline__ Tile in(int t, int r) const
+    {
+        const int upto = position[r] - t * kTile;
+        return Tile{upto, window ? upto - window : -1};
+    }
+    __device__ __forceinline__ bool sees(int key, int r) const { return key <= position[r] && !(window && key <= position[r] - window); }
+};
+template <int kGroups>
+struct Seen<kGroups, PagedTreeAttention> {       // see TreeRow; the tokens of a tile are 64 at most, one word
+    unsigned long long marks[kGroups];
+    int low[kGroups], base, last;
+    TreeEdges edges;
+    __device__ __forceinline__ void item(const PagedTreeAttention& a, const Item& it, int, int)
+    {
+        base = it.rows.base;
+        last = base + it.rows.n;
+        edges = tree_edges(a, it.rows);
+    }
+    __device__ __forceinline__ void row(const PagedTreeAttention& a, const Item& it, int r, int i)
+    {
+        const TreeRow t = tree_row(a, it.rows, i);
+        marks[r] = t.mask[0];
+        low[r] = t.low;
+    }
+    __device__ __forceinline__ int end() const { return last; }
+    __device__ __forceinline__ bool edge(int t) const { return t * kTile + kTile > edges.from || t * kTile < edges.upto; }
+    struct Tile {
+        uint32_t bits;
+        __device__ __forceinline__ bool operator()(int key) const { return bits >> key & 1; }
+    };
+    __device__ __forceinline__ Tile in(int t, int r) const
+    {
+        const int at = t * kTile - base;                      // of the tile's first key among the new ones
+        const uint32_t marked = at >= 64 || at <= -kTile ? 0u : (uint32_t)(at >= 0 ? marks[r] >> at : marks[r] << -at);
+        return Tile{((uint32_t)below(-at) | marked) & ~(uint32_t)below(low[r] - t * kTile)};
+    }
+    __device__ __forceinline__ bool sees(int key, int r) const { return in(key / kTile, r)(key & (kTile - 1)); }
+};
+
 // Tiles [t0, t1) of 32 keys through one wave; `ring`: LDS offset of its ring.
 // kOnePage: pages of 16 rows or more, which hold halves of tiles, so that their addresses are scalars.
-template <int kGroups, bool kOnePage>
+template <int kGroups, bool kOnePage, class A>
 __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, const bf16x8 (&q)[kGroups][4], int t0, int t1, uint32_t ring,
-                                       const int (&position)[kGroups], int pos_min, int pos_max, int window, float scale)
+                                       const Seen<kGroups, A>& seen, float scale)
 {
     const float top = hidden_infinity();
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
@@ -148,8 +206,7 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
             entries[2] = entries[3];
             entries[3] = entry_at(t + 4);
         }
-        // a tile in which some row sees a key that another one does not
-        const bool edge = t * kTile + kTile - 1 > pos_min || (window && t * kTile <= pos_max - window);
+        const bool edge = seen.edge(t);
         f32x4 s[kGroups][2];
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) s[r][0] = s[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -163,11 +220,11 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
         if (valid != 0xffffffffu || edge) {
 #pragma unroll
             for (int r = 0; r < kGroups; ++r) {
-                const int upto = position[r] - t * kTile, from = window ? upto - window : -1;
+                const auto sees = seen.in(t, r);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int key = 16 * (i >> 2) + 4 * g + (i & 3);
-                    s[r][i >> 2][i & 3] = (valid >> key & 1) && key <= upto && key > from ? s[r][i >> 2][i & 3] : -INFINITY;
+                    s[r][i >> 2][i & 3] = (valid >> key & 1) && sees(key) ? s[r][i >> 2][i & 3] : -INFINITY;
                 }
             }
         }
@@ -283,7 +340,7 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
                 const uint32_t u[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
 #pragma unroll
                 for (int r = 0; r < kGroups; ++r) {
-                    const bool sees = key <= position[r] && !(window && key <= position[r] - window);
+                    const bool sees = seen.sees(key, r);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (sees && (u[e] & 0x7f800000u) == 0x7f800000u) st.o[r][d][e] += __uint_as_float(u[e]);
@@ -309,8 +366,8 @@ __device__ __forceinline__ void store_row(const PagedAttention& a, int token, in
     if (a.lse && d == 0 && g == 0) a.lse[row] = some ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
 }
 
-template <int kGroups, bool kOnePage>
-__global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
+template <int kGroups, bool kOnePage, class A>
+__device__ __forceinline__ void attend(const A& a, const Tiling& tl, float* parts, Cut* cuts)
 {
     constexpr int kRows = 16 * kGroups;
     __shared__ __align__(256) unsigned char lds[kWaves * kRing + 2 * kWaves * kRows * 4];
@@ -334,15 +391,16 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
         if (first == last) continue;                       // (the share ends among the places in front)
         const bool whole = first == it.b0 && last == it.b1;
         const int tokens = min(it.rows.n - it.tile * tl.tokens, tl.tokens), tile_rows = tokens * G;
-        const int pos_min = it.rows.base + it.tile * tl.tokens, pos_max = pos_min + tokens - 1;
-        int token[kGroups], head[kGroups], position[kGroups];
+        Seen<kGroups, A> seen;
+        seen.item(a, it, it.tile * tl.tokens, tokens);
+        int token[kGroups], head[kGroups];
         bf16x8 q[kGroups][4];
 #pragma unroll
         for (int r = 0; r < kGroups; ++r) {
             const int row = min(16 * r + col, tile_rows - 1), in_tile = token_of_row(tl, row), i = it.tile * tl.tokens + in_tile;
             token[r] = it.rows.q0 + i;
             head[r] = h * G + row - in_tile * G;
-            position[r] = it.rows.base + i;
+            seen.row(a, it, r, i);
             const uint4* from = reinterpret_cast<const uint4*>(a.q + (long long)token[r] * a.q_stride + (long long)head[r] * kHeadDim);
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) q[r][ks] = __builtin_bit_cast(bf16x8, from[4 * ks + g]);
@@ -356,7 +414,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
         c.shift = a.c.page_shift;
         c.n_kv = a.c.n_kv;
         c.h = h;
-        c.end = min(pos_max + 1, room_of(a));
+        c.end = min(seen.end(), room_of(a));
         // the wave's tiles: a quarter of the share's
         const int t0 = first * kWaves + wave * (last - first), t1 = min(t0 + (last - first), c.end > 0 ? (c.end - 1) / kTile + 1 : 0);
         State<kGroups> st;
@@ -367,7 +425,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
 #pragma unroll
             for (int d = 0; d < 8; ++d) st.o[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        if (t0 < t1) stream<kGroups, kOnePage>(st, c, q, t0, t1, ring, position, pos_min, pos_max, a.window, a.scale_log2e);
+        if (t0 < t1) stream<kGroups, kOnePage, A>(st, c, q, t0, t1, ring, seen, a.scale_log2e);
 
         // The waves' sums meet.
         __syncthreads();
@@ -423,6 +481,17 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttent
         __syncthreads();
     }
     if (threadIdx.x == 0) cuts[share] = cut;
+}
+
+template <int kGroups, bool kOnePage>
+__global__ __launch_bounds__(64 * kWaves, 1) void paged_token_kernel(PagedAttention a, Tiling tl, float* parts, Cut* cuts)
+{
+    attend<kGroups, kOnePage>(a, tl, parts, cuts);
+}
+template <int kGroups, bool kOnePage>
+__global__ __launch_bounds__(64 * kWaves, 1) void paged_tree_token_kernel(PagedTreeAttention a, Tiling tl, float* parts, Cut* cuts)
+{
+    attend<kGroups, kOnePage>(a, tl, parts, cuts);
 }
 
 // One workgroup a cut, 16 rows and 16 dims: its waves take parts in turn, eight at a time, so that a cut of up to 32 parts costs one trip to memory.
@@ -493,17 +562,22 @@ __global__ __launch_bounds__(256) void paged_token_merge_kernel(PagedAttention a
     if (row < c.rows) store_row(a, c.q0 + row / group, c.head * group + row % group, o, M, L, d, g);
 }
 
-template <int kGroups>
-hipError_t launch(const PagedAttention& a, float* room, hipStream_t s)
+template <int kGroups, bool kOnePage>
+auto kernel_of(const PagedAttention&) { return paged_token_kernel<kGroups, kOnePage>; }
+template <int kGroups, bool kOnePage>
+auto kernel_of(const PagedTreeAttention&) { return paged_tree_token_kernel<kGroups, kOnePage>; }
+
+template <int kGroups, class A>
+hipError_t launch(const A& a, float* room, hipStream_t s)
 {
     const Tiling tl = tiling(a.n_q_heads / a.c.n_kv, 16 * kGroups, 0, 16 * kGroups, kWaves * kTile, 2, 1);
     Cut* cuts = reinterpret_cast<Cut*>(room);
     float* parts = room + kCutFloats;
-    const auto kernel = a.c.page_shift >= 4 ? paged_token_kernel<kGroups, true> : paged_token_kernel<kGroups, false>;
+    const auto kernel = a.c.page_shift >= 4 ? kernel_of<kGroups, true>(a) : kernel_of<kGroups, false>(a);
     hipLaunchKernelGGL(kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_token_merge_kernel<kGroups>), dim3(8 * kGroups * kWorkgroups), dim3(256), 0, s, a, tl.group, (const float*)parts, (const Cut*)cuts);
+    hipLaunchKernelGGL((paged_token_merge_kernel<kGroups>), dim3(8 * kGroups * kWorkgroups), dim3(256), 0, s, (const PagedAttention&)a, tl.group, (const float*)parts, (const Cut*)cuts);
     return hipGetLastError();
 }
 
@@ -511,9 +585,12 @@ hipError_t launch(const PagedAttention& a, float* room, hipStream_t s)
 
 size_t paged_token_floats(int rows) { return (size_t)2 * kWorkgroups * part_floats(rows / 16) + kCutFloats; }
 
-hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s)
+template <class A>
+static hipError_t launch_tokens(const A& a, int rows, float* room, hipStream_t s)
 {
     return rows == 16 ? launch<1>(a, room, s) : rows == 32 ? launch<2>(a, room, s) : rows == 64 ? launch<4>(a, room, s) : hipErrorInvalidValue;
 }
+hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s) { return launch_tokens(a, rows, room, s); }
+hipError_t launch_paged_tokens(const PagedTreeAttention& a, int rows, float* room, hipStream_t s) { return launch_tokens(a, rows, room, s); }
 
 }  // namespace mp
