@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmp.so")
-SOURCES = ["mp_api.hip", "mp_value.hip", "mp_stream.hip", "mp_stream_terms.hip", "mp_stream_dense.hip", "mp_stream8.hip", "mp_score.hip", "mp_index.hip", "mp_assign.hip", "mp_means.hip", "mp_cluster.hip", "mp_rotary.hip", "mp_norm_rotary.hip", "mp_paged_attn.hip", "mp_paged_chunk.hip", "mp_paged_token.hip", "mp_paged_tree.hip", "mp_paged_pool.hip", "mp_paged_api.hip"]
+SOURCES = ["mp_api.hip", "mp_value.hip", "mp_stream.hip", "mp_stream_terms.hip", "mp_stream_dense.hip", "mp_stream8.hip", "mp_score.hip", "mp_index.hip", "mp_assign.hip", "mp_means.hip", "mp_cluster.hip", "mp_rotary.hip", "mp_norm_rotary.hip", "mp_paged_attn.hip", "mp_paged_chunk.hip", "mp_paged_token.hip", "mp_paged_rows.hip", "mp_paged_tree.hip", "mp_paged_pool.hip", "mp_paged_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # scalar arguments in registers when a wave starts, instead of a first trip to a segment no one has read yet:
@@ -27,7 +27,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # mp_assign.hip: keep the MFMA accumulators in ordinary vector registers; the comparison code reads
 # every one of them, and copying them out of accumulation registers costs an instruction each
 # mp_paged_token.hip: the same; its 64-row kernel copied the accumulators back and forth, 500 instructions a tile
-EXTRA_FLAGS = {"mp_assign.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "mp_paged_token.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# mp_paged_rows.hip: the same
+EXTRA_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("mp_assign.hip", "mp_paged_token.hip", "mp_paged_rows.hip")}
 
 
 def _headers():

@@ -85,6 +85,9 @@ size_t paged_partial_floats(int n_tokens, int n_q_heads, int n_kv_heads, int n_s
 size_t paged_token_floats(int rows);
 hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s);
 hipError_t launch_paged_tokens(const PagedTreeAttention& a, int rows, float* room, hipStream_t s);
+hipError_t launch_paged_token_merge(const PagedAttention& a, int groups, const float* parts, const void* cuts, hipStream_t s);
+// The kernel for trees of up to `rows` query rows a KV head (64 or 128), in room for paged_token_floats(rows).
+hipError_t launch_paged_tree_rows(const PagedTreeAttention& a, int rows, float* room, hipStream_t s);
 size_t paged_chunk_floats();
 hipError_t launch_paged_chunks(const PagedAttention& a, int over, float* room, hipStream_t s);     // sequences of more than `over` query rows a head
 hipError_t launch_paged_chunks(const PagedTreeAttention& a, int over, float* room, hipStream_t s);

@@ -63,10 +63,27 @@ bool paged_line_fits(const PagedAttention& a)
 }
 bool paged_line_fits(const PagedTreeAttention& a) { return line_fits(a, 256 / (a.n_q_heads / a.c.n_kv), a.max_new); }
 
+static hipError_t launch_rows(const PagedTreeAttention& a, hipStream_t s, bool* done)
+{
+    const long long rows = (long long)a.max_new * (a.n_q_heads / a.c.n_kv);
+    const int most = rows <= 64 ? 64 : 128;
+    // (the workspace is that of paged_partial_floats, whichever kernel runs: of 33 rows on, it holds the parts of 64, and of 65 on more than those of 128)
+    *done = rows > 32 && rows <= 128 && paged_token_floats(most) <= paged_partial_floats(a.n_tokens, a.n_q_heads, a.c.n_kv, a.c.n_seqs, a.max_new);
+    return *done ? launch_paged_tree_rows(a, most, a.partials, s) : hipSuccess;
+}
+static hipError_t launch_rows(const PagedAttention&, hipStream_t, bool* done)
+{
+    *done = false;
+    return hipSuccess;
+}
+
 template <class A>
 static hipError_t launch_attention(const A& a, hipStream_t s)
 {
     if (a.n_tokens <= 0 || a.c.n_seqs <= 0) return hipSuccess;
+    bool done;
+    const hipError_t rows = launch_rows(a, s, &done);
+    if (done) return rows;
     Kernels k = kernels_of(a.n_tokens, a.n_q_heads / a.c.n_kv, a.c.n_seqs, a.max_new);
     if (k.chunks && !short_ones_apart(a)) k.tokens = 0;
     float* room = a.partials;

@@ -10,37 +10,15 @@
 // token over 4096 keys: 8.0 us and 4.9 for the merge, trips to memory one behind the other (lengths, page, keys, parts) and two launches.
 #include <type_traits>
 
-#include "mp_paged_plan.h"
+#include "mp_paged_tile.h"
 
 namespace mp {
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) unsigned char lds_byte;
-
 constexpr int kWaves = 4, kTile = 32;
 constexpr int kPiece = kTile * 256, kSlot = 2 * kPiece, kRing = 2 * kSlot;
-// A part: weighted values as the lanes hold them, then maxima, then sums.
-constexpr int part_floats(int groups) { return 16 * groups * kHeadDim + 2 * 16 * groups; }
 constexpr size_t kCutFloats = sizeof(Cut) / sizeof(float) * kWorkgroups;
-
-__device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds_off)
-{
-    // (the LDS address is the same in all lanes; lane i's bytes go to it + 16 i)
-    auto* dst = reinterpret_cast<__attribute__((address_space(3))) uint32_t*>((uintptr_t)lds_off);
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src, dst, 16, 0, 2);      // (2: non-temporal)
-}
-template <int N>
-__device__ __forceinline__ void wait_vm()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 
 template <int kGroups>
 struct State {
@@ -354,18 +332,6 @@ __device__ __forceinline__ void stream(State<kGroups>& st, const Source& c, cons
     tile(t, std::integral_constant<int, 0>{});
 }
 
-__device__ __forceinline__ void store_row(const PagedAttention& a, int token, int head, const f32x4& o, float m, float l, int d, int g)
-{
-    const bool some = l != 0.f;              // (0: no key, or none of any weight; NaN, of a logit that is NaN or +inf, stays)
-    const float f = some ? 1.f / l : 0.f;
-    const long long row = (long long)token * a.n_q_heads + head;
-    bf16x4 w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = (__bf16)(some ? o[e] * f : 0.f);
-    *reinterpret_cast<bf16x4*>(a.out + row * kHeadDim + 16 * d + 4 * g) = w;
-    if (a.lse && d == 0 && g == 0) a.lse[row] = some ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
-}
-
 template <int kGroups, bool kOnePage, class A>
 __device__ __forceinline__ void attend(const A& a, const Tiling& tl, float* parts, Cut* cuts)
 {
@@ -575,13 +541,18 @@ hipError_t launch(const A& a, float* room, hipStream_t s)
     float* parts = room + kCutFloats;
     const auto kernel = a.c.page_shift >= 4 ? kernel_of<kGroups, true>(a) : kernel_of<kGroups, false>(a);
     hipLaunchKernelGGL(kernel, dim3(kWorkgroups), dim3(64 * kWaves), 0, s, a, tl, parts, cuts);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_token_merge_kernel<kGroups>), dim3(8 * kGroups * kWorkgroups), dim3(256), 0, s, (const PagedAttention&)a, tl.group, (const float*)parts, (const Cut*)cuts);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : launch_paged_token_merge(a, kGroups, parts, cuts, s);
 }
 
 }  // namespace
+
+hipError_t launch_paged_token_merge(const PagedAttention& a, int groups, const float* parts, const void* cuts, hipStream_t s)
+{
+    const auto kernel = groups == 1 ? paged_token_merge_kernel<1> : groups == 2 ? paged_token_merge_kernel<2> : groups == 4 ? paged_token_merge_kernel<4> : paged_token_merge_kernel<8>;
+    hipLaunchKernelGGL(kernel, dim3(8 * groups * kWorkgroups), dim3(256), 0, s, a, a.n_q_heads / a.c.n_kv, parts, (const Cut*)cuts);
+    return hipGetLastError();
+}
 
 size_t paged_token_floats(int rows) { return (size_t)2 * kWorkgroups * part_floats(rows / 16) + kCutFloats; }
 

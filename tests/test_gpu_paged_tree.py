@@ -172,6 +172,20 @@ def test_infinite_values_reach_the_tokens_that_mark_them(new, G):
     assert out.isfinite().all()
 
 
+@pytest.mark.parametrize("new,G", [(1, 4), (4, 4), (8, 2), (5, 4), (8, 4), (9, 4), (16, 4), (17, 4), (32, 4), (33, 4), (63, 4), (100, 8)])
+@pytest.mark.parametrize("seqs", [1, 3])
+def test_nothing_is_written_past_the_workspace(new, G, seqs):
+    mp = _mp()
+    b = Batch([new] * seqs, [2000 + new] * seqs, 2, 16)
+    n = mp.mp_paged_workspace_bytes(b.T, 2 * G, 2, seqs, new)
+    whole = torch.full((n + (64 << 20),), 85, dtype=torch.uint8, device="cuda")       # (room behind it for the largest kernel's parts)
+    q = _rows(b.T, 2 * G, 3)
+    out = b.paged().mp_paged_tree_attention(q, _mask(b, _trees(b.new), -(-new // 64)), max_new=new, workspace=whole[:n])
+    assert (whole[n:] == 85).all()
+    want, _, ob, _ = tree_attention(b, q, _trees(b.new))
+    check(out, want, ob, "out")
+
+
 def test_workspace_that_is_shared_and_repeated_calls():
     mp = _mp()
     b = Batch([24, 9, 24], [3000, 100, 777], 4, 16)
