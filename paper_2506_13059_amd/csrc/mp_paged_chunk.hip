@@ -513,32 +513,51 @@ __global__ __launch_bounds__(64) void paged_chunk_merge_kernel(PagedAttention a,
     if (c.parts == 0 || wave * 32 >= c.rows) return;
     auto part = [&](int g) { return parts + (2ll * (share + g) + (g == 0 ? c.slot : 0)) * kPartFloats; };
     const int at_m = kRows * kHeadDim + wave * 32 + (lane & 31);
-    float m = -INFINITY;
+    // (the first parts' rows are asked for before the maximum of all is known: most cuts have two or three)
+    constexpr int kAtOnce = 4;
+    float m[kAtOnce], l_of[kAtOnce];
+    f32x4 y[kAtOnce][4];
+    auto ask = [&](int g0) {
+#pragma unroll
+        for (int g = 0; g < kAtOnce; ++g) {
+            if (g0 + g >= c.parts) break;
+            const float* p = part(g0 + g);
+            m[g] = p[at_m];
+            l_of[g] = p[at_m + kRows];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[g][j] = reinterpret_cast<const f32x4*>(p)[(wave * 16 + 4 * d + j) * 64 + lane];
+        }
+    };
+    ask(0);
+    float top = -INFINITY;
 #pragma unroll 4
-    for (int g = 0; g < c.parts; ++g) m = fmaxf(m, part(g)[at_m]);
-    const float ms = m == -INFINITY ? 0.f : m;
+    for (int g = kAtOnce; g < c.parts; ++g) top = fmaxf(top, part(g)[at_m]);
+#pragma unroll
+    for (int g = 0; g < kAtOnce; ++g)
+        if (g < c.parts) top = fmaxf(top, m[g]);
+    const float ms = top == -INFINITY ? 0.f : top;
     float l = 0.f;
     f32x4 o[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int g = 0; g < c.parts; ++g) {
-        const float* p = part(g);
-        const float f = __builtin_amdgcn_exp2f(p[at_m] - ms);
-        l = fmaf(p[at_m + kRows], f, l);
-        const f32x4* from = reinterpret_cast<const f32x4*>(p) + (wave * 16 + 4 * d) * 64 + lane;
+    for (int g0 = 0; g0 < c.parts; g0 += kAtOnce) {
+        if (g0) ask(g0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const f32x4 w = from[j * 64];
+        for (int g = 0; g < kAtOnce; ++g) {
+            if (g0 + g >= c.parts) break;
+            const float f = __builtin_amdgcn_exp2f(m[g] - ms);
+            l = fmaf(l_of[g], f, l);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[j][e] = fmaf(w[e], f, o[j][e]);
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][e] = fmaf(y[g][j][e], f, o[j][e]);
         }
     }
     const int r = wave * 32 + (lane & 31);
     if (r >= c.rows) return;
     const long long row = (long long)(c.q0 + r / group) * a.n_q_heads + c.head * group + r % group;
     store_dims(a, row, d, half, o, l);
-    if (a.lse && d == 0 && half == 0) a.lse[row] = lse_of(m, l);
+    if (a.lse && d == 0 && half == 0) a.lse[row] = lse_of(top, l);
 }
 
 constexpr size_t kCutFloats = sizeof(Cut) / sizeof(float) * kWorkgroups;

@@ -148,7 +148,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
         // (here, for otherwise the wait for them is put into the loop, and there it is one for all loads to LDS)
         asm volatile("" : "+v"(q[0]), "+v"(q[1]), "+v"(q[2]), "+v"(q[3]), "+v"(marks0), "+v"(marks1));
         const TreeEdges edges = tree_edges(a, it.rows);
-        auto edge = [&](int block) { return block * kKeys + kKeys > edges.from || block * kKeys < edges.upto; };
+        auto edge = [&](int block) { return block * kKeys + kKeys - 1 >= edges.from || block * kKeys < edges.upto; };
         // a bit for each key of a block
         auto attended = [&](int block) {
             const int at = block * kKeys - base, by = at & 63;

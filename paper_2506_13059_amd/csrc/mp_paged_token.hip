@@ -76,7 +76,7 @@ struct Seen<kGroups, PagedTreeAttention> {       // see TreeRow; the tokens of a
         low[r] = t.low;
     }
     __device__ __forceinline__ int end() const { return last; }
-    __device__ __forceinline__ bool edge(int t) const { return t * kTile + kTile > edges.from || t * kTile < edges.upto; }
+    __device__ __forceinline__ bool edge(int t) const { return t * kTile + kTile - 1 >= edges.from || t * kTile < edges.upto; }
     struct Tile {
         uint32_t bits;
         __device__ __forceinline__ bool operator()(int key) const { return bits >> key & 1; }
@@ -473,11 +473,13 @@ __global__ __launch_bounds__(256) void paged_token_merge_kernel(PagedAttention a
     if (c.parts == 0 || 16 * r >= c.rows) return;
     float M = -INFINITY, L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = wave; i0 < c.parts; i0 += 32) {
-        float m[8], l[8];
-        f32x4 y[8];
+    // The wave's parts from i0 on, every fourth, up to kAtOnce of them on their way together.
+    auto take = [&](int i0, auto at_once) {
+        constexpr int kAtOnce = decltype(at_once)::value;
+        float m[kAtOnce], l[kAtOnce];
+        f32x4 y[kAtOnce];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kAtOnce; ++k) {
             const int i = min(i0 + 4 * k, c.parts - 1);
             const float* p = parts + (2ll * (share + i) + (i == 0 ? c.slot : 0)) * part_floats(kGroups);
             m[k] = p[kRows * kHeadDim + 16 * r + col];
@@ -486,7 +488,7 @@ __global__ __launch_bounds__(256) void paged_token_merge_kernel(PagedAttention a
         }
         float n = M;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kAtOnce; ++k) {
             if (i0 + 4 * k >= c.parts) m[k] = -INFINITY;
             n = fmaxf(n, m[k]);
         }
@@ -495,7 +497,7 @@ __global__ __launch_bounds__(256) void paged_token_merge_kernel(PagedAttention a
         L *= before;
         o *= before;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kAtOnce; ++k) {
             const float f = __builtin_amdgcn_exp2f(m[k] - base);
             if (i0 + 4 * k < c.parts) {
                 L = fmaf(l[k], f, L);
@@ -503,6 +505,12 @@ __global__ __launch_bounds__(256) void paged_token_merge_kernel(PagedAttention a
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(y[k][e], f, o[e]);
             }
         }
+    };
+    // (many short items are cut into two or three parts, of which eight loads a wave would bring most several times)
+    if (c.parts <= 4) {
+        if (wave < c.parts) take(wave, std::integral_constant<int, 1>{});
+    } else {
+        for (int i0 = wave; i0 < c.parts; i0 += 32) take(i0, std::integral_constant<int, 8>{});
     }
     sm_o[wave][lane] = o;
     if (lane < 16) {
