@@ -6,6 +6,7 @@
 // factor 1 / sqrt() is a row's, so it multiplies last; where all heads have the same weights these go into the cosines and sines of a token, once for all of its rows.
 //
 // Copies, bound by memory, or by a launch and its trips to memory where there are few tokens.
+#include "mp_launch.h"
 #include "mp_turn.h"
 
 namespace mp {
@@ -218,11 +219,10 @@ hipError_t launch_norm_rotary(const Rotation& rot, const HeadNorm& norm, const T
     const int rows = rows_of_a_wave(n_tokens, x.n_heads), parts = (x.n_heads + rows - 1) / rows;
     const long long blocks = ((long long)n_tokens * parts + kWaves - 1) / kWaves;
     const bool once = past_caches((long long)n_tokens * x.n_heads * ((out != nullptr) + (out_lookup != nullptr)));
-    const auto kernel = norm.stride ? (once ? norm_rotary_kernel<true, true> : norm_rotary_kernel<false, true>)
-                                    : (once ? norm_rotary_kernel<true, false> : norm_rotary_kernel<false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, rot, norm, x.p, x.stride, positions, out, out_stride, out_lookup,
-                       lookup_position, n_tokens, x.n_heads, rows, parts);
-    return hipGetLastError();
+    const auto on = norm.stride ? (once ? Launch<norm_rotary_kernel<true, true>>::on : Launch<norm_rotary_kernel<false, true>>::on)
+                                : (once ? Launch<norm_rotary_kernel<true, false>>::on : Launch<norm_rotary_kernel<false, false>>::on);
+    return on(dim3((unsigned)blocks), dim3(64 * kWaves), s, rot, norm, x.p, x.stride, positions, out, out_stride, out_lookup, lookup_position, n_tokens, x.n_heads, rows,
+              parts);
 }
 
 hipError_t launch_paged_append_norm(const PagedKv& c, const Rotation& rot, const HeadNorm& q_norm, const HeadNorm& k_norm, const int32_t* positions,
@@ -232,10 +232,9 @@ hipError_t launch_paged_append_norm(const PagedKv& c, const Rotation& rot, const
     const int groups = (q.n_heads + 3) / 4 + 2 * ((c.n_kv + 3) / 4);
     const int per = rows_of_a_wave(n_tokens, 4 * groups) / 4, parts = (groups + per - 1) / per;
     const long long blocks = ((long long)n_tokens * parts + kWaves - 1) / kWaves;
-    const auto kernel = past_caches((long long)n_tokens * (q.n_heads + 2 * c.n_kv)) ? paged_append_norm_kernel<true> : paged_append_norm_kernel<false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, c, rot, q_norm, k_norm, positions, q.p, q.stride, q_out, k.p, k.stride, v.p,
-                       v.stride, n_tokens, q.n_heads, per, parts);
-    return hipGetLastError();
+    const auto on = past_caches((long long)n_tokens * (q.n_heads + 2 * c.n_kv)) ? Launch<paged_append_norm_kernel<true>>::on : Launch<paged_append_norm_kernel<false>>::on;
+    return on(dim3((unsigned)blocks), dim3(64 * kWaves), s, c, rot, q_norm, k_norm, positions, q.p, q.stride, q_out, k.p, k.stride, v.p, v.stride, n_tokens, q.n_heads, per,
+              parts);
 }
 
 }  // namespace mp

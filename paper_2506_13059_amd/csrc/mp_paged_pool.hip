@@ -6,6 +6,7 @@
 //
 // One workgroup, for everything hangs on two running sums over the sequences: bound by its trips to memory one behind the other.  The maps of many tokens are a launch of their own.
 #include "mp_device.h"
+#include "mp_launch.h"
 #include "mp_paged.h"
 
 namespace mp {
@@ -379,12 +380,10 @@ hipError_t launch_paged_reserve(const PagePool& p, const int32_t* n_new, const i
     const bool apart = rows.n_rows > kMapped;
     StepRows here = rows;
     if (apart) here.n_rows = 0;
-    const auto kernel = p.n_seqs <= kThreads ? paged_reserve_once_kernel : paged_reserve_kernel;
-    hipLaunchKernelGGL(kernel, dim3(1), dim3(kThreads), 0, s, p, n_new, keep, granted, here);
-    const hipError_t e = hipGetLastError();
+    const auto on = p.n_seqs <= kThreads ? Launch<paged_reserve_once_kernel>::on : Launch<paged_reserve_kernel>::on;
+    const hipError_t e = on(dim3(1), dim3(kThreads), s, p, n_new, keep, granted, here);
     if (e != hipSuccess || !apart) return e;
-    hipLaunchKernelGGL(paged_map_kernel, dim3((unsigned)(((long long)rows.n_rows + 255) / 256)), dim3(256), 0, s, p, rows);
-    return hipGetLastError();
+    return Launch<paged_map_kernel>::on(dim3((unsigned)(((long long)rows.n_rows + 255) / 256)), dim3(256), s, p, rows);
 }
 
 }  // namespace mp

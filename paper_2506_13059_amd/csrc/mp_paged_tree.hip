@@ -3,6 +3,7 @@
 // Tokens of a tree are in an order in which each follows its parent.  A token's mask marks itself and its ancestors, and its position is that of its sequence's older keys and
 // the length of its path.  Both kernels are a few trips to memory.
 #include "mp_device.h"
+#include "mp_launch.h"
 #include "mp_paged.h"
 
 namespace mp {
@@ -112,18 +113,16 @@ hipError_t launch_paged_tree_plan(const PagedKv& c, const int32_t* parents, int 
     if (n_tokens <= 0 || c.n_seqs <= 0) return hipSuccess;
     int size = 1;
     while (size < words) size *= 2;
-    const auto kernel = size == 1 ? paged_tree_plan_kernel<1> : size == 2 ? paged_tree_plan_kernel<2> : size == 4 ? paged_tree_plan_kernel<4>
-                      : size == 8 ? paged_tree_plan_kernel<8> : paged_tree_plan_kernel<16>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)c.n_seqs), dim3(64 * size), 0, s, c, parents, n_tokens, words, (unsigned long long*)mask, positions);
-    return hipGetLastError();
+    const auto on = size == 1 ? Launch<paged_tree_plan_kernel<1>>::on : size == 2 ? Launch<paged_tree_plan_kernel<2>>::on : size == 4 ? Launch<paged_tree_plan_kernel<4>>::on
+                  : size == 8 ? Launch<paged_tree_plan_kernel<8>>::on : Launch<paged_tree_plan_kernel<16>>::on;
+    return on(dim3((unsigned)c.n_seqs), dim3(64 * size), s, c, parents, n_tokens, words, (unsigned long long*)mask, positions);
 }
 
 hipError_t launch_paged_tree_keep(const PagedKv& c, const uint64_t* mask, int words, const int32_t* leaf, int n_tokens, int32_t* keep, hipStream_t s)
 {
     if (c.n_seqs <= 0) return hipSuccess;
     const long long blocks = (2ll * c.n_kv * c.n_seqs + kWaves - 1) / kWaves;
-    hipLaunchKernelGGL(paged_tree_keep_kernel, dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, c, (const unsigned long long*)mask, words, leaf, n_tokens, keep);
-    return hipGetLastError();
+    return Launch<paged_tree_keep_kernel>::on(dim3((unsigned)blocks), dim3(64 * kWaves), s, c, (const unsigned long long*)mask, words, leaf, n_tokens, keep);
 }
 
 }  // namespace mp
