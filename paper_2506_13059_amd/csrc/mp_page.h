@@ -44,6 +44,36 @@ MP_PAGE_FN void blocks_of(int base, int i0, int i1, int window, int room, int un
     if (*b1 <= *b0) *b1 = *b0 + 1;
 }
 
+// The lowest n of 64 bits.
+MP_PAGE_FN unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
+
+// A row of a tree attends the keys of its sequence that are older than the `n` new ones, `base` of them, and the new ones that its mask marks (bit i % 64 of word i / 64: the i-th); a window
+// leaves it the last ones of all these.  Either way it attends the keys from a first one on, `low`, that are older or marked.
+MP_PAGE_FN int tree_low(const unsigned long long* mask, int words, int base, int n, int window)
+{
+    if (window <= 0) return 0;
+    int left = window;
+    const int used = (int)(((long long)n + 63) >> 6);
+    for (int w = (words < used ? words : used) - 1; w >= 0; --w) {
+        unsigned long long m = mask[w] & below(n - 64 * w);
+        const int marked = __builtin_popcountll(m);
+        if (marked >= left) {                       // (it attends no older key)
+            for (; left > 1; --left) m &= ~(1ull << (63 - __builtin_clzll(m)));
+            return base + 64 * w + 63 - __builtin_clzll(m);
+        }
+        left -= marked;
+    }
+    return (base > left ? base : left) - left;
+}
+// Which of the 64 keys from `first` on such a row attends: a bit for each.  words: of its mask that count.
+MP_PAGE_FN unsigned long long tree_keys(const unsigned long long* mask, int words, int low, int base, int first)
+{
+    const int at = first - base, w = at >> 6, by = at & 63;      // of the first key among the new ones
+    unsigned long long marked = w >= 0 && w < words ? mask[w] >> by : 0ull;
+    if (by && w + 1 >= 0 && w + 1 < words) marked |= mask[w + 1] << (64 - by);
+    return (below(-at) | marked) & ~below(low - first);
+}
+
 // Work is cut into equal shares of blocks, a workgroup each, without regard to where an item (a tile of rows of a head) ends; the first
 // and the last item of a share may be parts.  Which workgroup holds what of the item [x0, x1):
 struct Parts {

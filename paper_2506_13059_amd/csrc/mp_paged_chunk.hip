@@ -162,15 +162,6 @@ __device__ __forceinline__ void store_part(float* part, const Softmax& st, float
     }
 }
 
-// Which keys of a block a row of a tree attends (see TreeRow), `base` of them older than the new ones: a bit for each.
-__device__ __forceinline__ unsigned long long tree_keys(const TreeRow& row, int words, int base, int block)
-{
-    const int at = block * kKeys - base, w = at >> 6, by = at & 63;      // of the block's first key among the new ones
-    unsigned long long marked = w >= 0 && w < words ? row.mask[w] >> by : 0ull;
-    if (by && w + 1 >= 0 && w + 1 < words) marked |= row.mask[w + 1] << (64 - by);
-    return (below(-at) | marked) & ~below(row.low - block * kKeys);
-}
-
 // kOnePage: pages of eight rows or more.  (Smaller ones take addresses a lane, and eight registers more than there are: 2048 tokens at 32K 1.06 ms for 1.02.)
 template <bool kOnePage, class A>
 __device__ __forceinline__ void attend(const A& a, const Tiling& tl, float* parts, Cut* cuts)
@@ -399,7 +390,7 @@ __device__ __forceinline__ void attend(const A& a, const Tiling& tl, float* part
                     // keys (from, upto] of the block, those that are there; bit k of `see` for key 4 half + k
                     unsigned long long keys;
                     if constexpr (kTree) {
-                        keys = tree_keys(row, words, it.rows.base, t);
+                        keys = tree_keys(row.mask, words, row.low, it.rows.base, t * kKeys);
                     } else {
                         const int upto = position - t * kKeys, from = a.window ? upto - a.window : -1;
                         keys = below(upto + 1) & ~below(from + 1);
@@ -459,7 +450,7 @@ __device__ __forceinline__ void attend(const A& a, const Tiling& tl, float* part
                         const int key = t * kKeys + __ffsll((long long)odd) - 1;
                         const int page = __builtin_amdgcn_readfirstlane(page_of(entries, a.c.table_stride, a.c.n_pages, a.c.page_shift, key));
                         bool sees = key <= position && !(a.window && key <= position - a.window);
-                        if constexpr (kTree) sees = tree_keys(row, words, it.rows.base, t) >> (key & (kKeys - 1)) & 1;
+                        if constexpr (kTree) sees = tree_keys(row.mask, words, row.low, it.rows.base, t * kKeys) >> (key & (kKeys - 1)) & 1;
                         const uint2* from = reinterpret_cast<const uint2*>(a.c.V + row_of(max(page, 0), h, a.c.n_kv, a.c.page_shift, key) * kHeadDim);
 #pragma unroll
                         for (int d = 0; d < 4; ++d)

@@ -82,38 +82,19 @@ __device__ __forceinline__ void blocks_of_tile(const PagedTreeAttention& a, cons
     blocks_of(r.base - 1, 0, r.n, a.window, room_of(a), tl.unit, b0, b1);
 }
 
-// What a query row attends: keys that are older than the new ones, from the row's first on (one key behind another, the last of them and the row's marks fill the window), and marked ones.
+// What a query row of a tree attends, see tree_keys.
 struct TreeRow {
     const unsigned long long* mask;
-    int low;                  // first key; if it is no older one, marks before it do not count
+    int low;
 };
 __device__ __forceinline__ TreeRow tree_row(const PagedTreeAttention& a, const SequenceRows& r, int i)
 {
-    TreeRow t{a.mask + (long long)(r.q0 + i) * a.words, 0};
-    if (a.window > 0) {
-        int left = a.window;
-        t.low = -1;
-        for (int w = min(a.words, (r.n + 63) >> 6) - 1; w >= 0; --w) {
-            const int in = r.n - 64 * w;
-            unsigned long long m = t.mask[w];
-            if (in < 64) m &= (1ull << in) - 1ull;
-            const int n = __popcll(m);
-            if (n >= left) {
-                while (--left > 0) m &= ~(1ull << (63 - __clzll((long long)m)));
-                t.low = r.base + 64 * w + 63 - __clzll((long long)m);
-                break;
-            }
-            left -= n;
-        }
-        if (left > 0) t.low = max(r.base, left) - left;
-    }
-    return t;
+    const unsigned long long* mask = a.mask + (long long)(r.q0 + i) * a.words;
+    return TreeRow{mask, tree_low(mask, a.words, r.base, r.n, a.window)};
 }
-// The lowest n of 64 bits.
-__device__ __forceinline__ unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
-// Keys of a sequence that are attended by all of its rows or by none lie before the first of these and behind the second, see edges.
+// Keys of a sequence before `upto` are not seen by some of its rows (a window's), those from `from` on may be new ones; all rows see what lies between.
 struct TreeEdges {
-    int upto, from;           // keys before `upto` are not seen by some rows (a window's), keys from `from` on may be new ones
+    int upto, from;
 };
 __device__ __forceinline__ TreeEdges tree_edges(const PagedTreeAttention& a, const SequenceRows& r)
 {
