@@ -12,20 +12,26 @@ namespace {
 constexpr int kKeys = 64, kRing = 4;
 constexpr int kHalf = 2 * 32 * 256, kBlockBytes = 2 * kHalf, kValues = 32 * 256;      // LDS: 32 keys and their values, and 32 more
 
-__device__ __forceinline__ u32x4 lds_read16(uint32_t at)
+// 16 bytes at `at` and each 1024 behind.
+__device__ __forceinline__ void lds_read(u32x4 (&w)[2], uint32_t at)
 {
-    u32x4 w;
-    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(at) : "memory");
-    return w;
+    asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:1024\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w[0]), "=&v"(w[1]) : "v"(at) : "memory");
 }
-__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 w) { asm volatile("ds_write_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" ::"v"(at), "v"(w) : "memory"); }
+__device__ __forceinline__ void lds_read(u32x4 (&w)[4], uint32_t at)
+{
+    asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %4 offset:3072\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3])
+                 : "v"(at)
+                 : "memory");
+}
+// (this and the next: waited for where the waves meet)
+__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 w) { asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(w) : "memory"); }
 __device__ __forceinline__ unsigned long long lds_read8(uint32_t at)        // the same in all lanes
 {
     unsigned long long w;
     asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(at) : "memory");
     return (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(w >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)w);
 }
-// (waited for where the waves meet)
 template <int kBytes>
 __device__ __forceinline__ void lds_write_bits(uint32_t at, uint32_t v)
 {
@@ -164,22 +170,23 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
             const bool at_edge = edge(block);
             const int place = block & (kRing - 1);
             if (there != (1u << kBring) - 1u || at_edge) {
+                const uint32_t at = wave_at + (uint32_t)(place * kBlockBytes) + kValues + lane * 16;
+                u32x4 w[kLoads];
+                lds_read(w, at);
 #pragma unroll
                 for (int e = 0; e < kLoads; ++e) {
-                    const uint32_t at = wave_at + (uint32_t)(place * kBlockBytes) + kValues + e * 1024 + lane * 16;
-                    u32x4 w = lds_read16(at);
                     bool off_range = false;
                     if (!(there >> (4 * e + g) & 1)) {
-                        w = u32x4{0u, 0u, 0u, 0u};
+                        w[e] = u32x4{0u, 0u, 0u, 0u};
                     } else if (at_edge) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const bool lo = (w[k] & 0x7f80u) == 0x7f80u, hi = (w[k] & 0x7f800000u) == 0x7f800000u;
+                            const bool lo = (w[e][k] & 0x7f80u) == 0x7f80u, hi = (w[e][k] & 0x7f800000u) == 0x7f800000u;
                             off_range |= lo | hi;
-                            w[k] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+                            w[e][k] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
                         }
                     }
-                    lds_write16(at, w);
+                    lds_write16(at + e * 1024, w[e]);
                     const unsigned long long in = __ballot(off_range);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) odd |= (uint32_t)((in >> (16 * k) & 0xffff) != 0) << (4 * e + k);
