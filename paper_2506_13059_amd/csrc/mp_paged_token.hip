@@ -628,7 +628,9 @@ constexpr int kManyItems = 128;      // sequences times KV heads
 template <int kGroups>
 static hipError_t merge(const PagedAttention& a, const float* parts, const Cut* cuts, hipStream_t s)
 {
-    const auto kernel = kGroups >= 4 && (long long)a.c.n_seqs * a.c.n_kv >= kManyItems ? paged_token_merge_few_kernel<kGroups> : paged_token_merge_kernel<kGroups>;
+    auto kernel = paged_token_merge_kernel<kGroups>;
+    if constexpr (kGroups >= 4)
+        if ((long long)a.c.n_seqs * a.c.n_kv >= kManyItems) kernel = paged_token_merge_few_kernel<kGroups>;
     hipLaunchKernelGGL(kernel, dim3(8 * kGroups * kWorkgroups), dim3(256), 0, s, a, a.n_q_heads / a.c.n_kv, parts, cuts);
     return hipGetLastError();
 }
@@ -640,12 +642,14 @@ hipError_t launch_paged_token_merge(const PagedAttention& a, int groups, const f
 
 size_t paged_token_floats(int rows) { return (size_t)2 * kWorkgroups * part_floats(rows / 16) + kCutFloats; }
 
-template <class A>
-static hipError_t launch_tokens(const A& a, int rows, float* room, hipStream_t s)
+hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s)
 {
     return rows == 16 ? launch<1>(a, room, s) : rows == 32 ? launch<2>(a, room, s) : rows == 64 ? launch<4>(a, room, s) : hipErrorInvalidValue;
 }
-hipError_t launch_paged_tokens(const PagedAttention& a, int rows, float* room, hipStream_t s) { return launch_tokens(a, rows, room, s); }
-hipError_t launch_paged_tokens(const PagedTreeAttention& a, int rows, float* room, hipStream_t s) { return launch_tokens(a, rows, room, s); }
+// (more rows of a tree: mp_paged_rows.hip)
+hipError_t launch_paged_tokens(const PagedTreeAttention& a, int rows, float* room, hipStream_t s)
+{
+    return rows == 16 ? launch<1>(a, room, s) : rows == 32 ? launch<2>(a, room, s) : hipErrorInvalidValue;
+}
 
 }  // namespace mp
