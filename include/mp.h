@@ -575,7 +575,9 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
  * Of a sequence, the first 64 * mask_words new tokens have results; other rows are left as they were.  The pages are not looked at.  Errors: MP_EINVAL, MP_EHIP.
  *
  * mp_paged_tree_attention -- every new token attends the keys of its sequence that are older than the new ones, and the new ones that its mask marks (any, also
- * such as stand behind it; itself only if it is marked).  window: of all these, the last `window` keys.  Other arguments, workspace, results and errors as of mp_paged_attention.
+ * such as stand behind it; itself only if it is marked).  window: of all these, the last `window` keys (marks, whether or not their pages are
+ * there, count first).  Other arguments, workspace, results and errors as of mp_paged_attention; probabilities have two parts where max_new * G <= 32, and in large batches with max_new * G > 128 for
+ * sequences of up to 16 query rows a KV head.
  *
  * mp_paged_tree_keep -- the rows of an accepted path moved together: of every sequence, the new tokens that the mask of its new token leaf[b] marks become the first of the new
  * ones, in their order, keys and values.  Rows without a page, before or after, are not moved; the rest of the rows is left as it was.

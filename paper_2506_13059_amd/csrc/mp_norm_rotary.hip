@@ -5,7 +5,8 @@
 // the mean over the 128 dimensions of a row, R(p) as in mp_rotary.hip.  The sum of squares, the weights and the rotation are fp32, and the result is rounded to bf16 once.  The
 // factor 1 / sqrt() is a row's, so it multiplies last; where all heads have the same weights these go into the cosines and sines of a token, once for all of its rows.
 //
-// Copies, bound by memory, or by a launch and its trips to memory where there are few tokens.
+// Copies, bound by memory, or by a launch and its trips to memory where there are few tokens: a decode step's 16 tokens of 32 heads at two positions 4.5 us on the device, 16 tokens' append 5.3; five prompts' append
+// (486 MB read and written, weights of each head) 97 us, 5.0 TB/s, as a large copy.
 #include "mp_launch.h"
 #include "mp_turn.h"
 

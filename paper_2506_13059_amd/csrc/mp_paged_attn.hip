@@ -63,6 +63,8 @@ bool paged_line_fits(const PagedAttention& a)
 }
 bool paged_line_fits(const PagedTreeAttention& a) { return line_fits(a, 256 / (a.n_q_heads / a.c.n_kv), a.max_new); }
 
+// Trees whose sequences have 33 to 128 query rows a KV head at most run in a kernel for them alone, short sequences among them (mp_paged_rows.hip says what it and the others take).  Up to 32, that for
+// few tokens reads faster and has probabilities in two parts: 8 tokens each of 8 sequences of up to 30K 110 us, 5.7 TB/s, where 12 each have 5.4 in the other.
 static hipError_t launch_rows(const PagedTreeAttention& a, hipStream_t s, bool* done)
 {
     const long long rows = (long long)a.max_new * (a.n_q_heads / a.c.n_kv);

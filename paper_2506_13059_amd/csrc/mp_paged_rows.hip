@@ -2,7 +2,10 @@
 //
 // Four or eight waves of 16 query rows each meet the same keys: 64 of them and their values at a time go straight to LDS (global_load_lds, 16 bytes a lane) into a ring of four
 // blocks, one in use and three on their way, and the waves meet behind each.  S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_16x16x32_bf16 as in mp_paged_token.hip; a wave's rows are
-// its own, so nothing is put together in the workgroup.
+// its own, so nothing is put together in the workgroup.  Bound by memory, or by trips to it and to instructions: a third of the code of mp_paged_token.hip for 64 rows, where each wave has all rows and keys of its own.
+//
+// By this and by what ran before (that one up to 64 rows, mp_paged_chunk.hip), 8 KV heads of four, us: 12 tokens over 4096 keys 16.8 and 22.4, 24 over as many 20 and 23.6; 12 each of 8 sequences of up to 30K 81 and
+// 87 (5.4 TB/s), 24 each 106 and 124, 32 each 91 and 102; 12 each of 32 of up to 2K 38 and 62, 24 each 46.8 and 46.9.  Two groups of rows a wave, for up to 256, took 8 to 10 % longer than chunks.
 #include "mp_paged_tile.h"
 
 namespace mp {
