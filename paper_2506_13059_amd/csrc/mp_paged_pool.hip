@@ -5,7 +5,7 @@
 // sequence; the first that finds too few gets no tokens, and neither does any behind it that needs pages.
 //
 // One workgroup, for everything hangs on two running sums over the sequences: bound by its trips to memory one behind the other.  The maps of many tokens are a launch of their own.  64 sequences of up to
-// eight tokens 6.3 us; 512 of which 64 give 4096 pages back and take as many 9.3, and 3.6 for the maps of their 50 thousand rows.
+// eight tokens 4.8 us; 512 of which 64 give 4096 pages back and take as many 9.2, and 3.6 for the maps of their 50 thousand rows.
 #include "mp_device.h"
 #include "mp_launch.h"
 #include "mp_paged.h"
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void paged_reserve_kernel(PagePool p, con
 }
 
 // Up to a thread a sequence: what the kernel below does, with what one step hands to the next in LDS, so that three trips to memory follow one another (lengths; entries that go back; the stack's top
-// and entries of rows on pages that were there) instead of nine: a step of 64 sequences 9.4 -> 6.4 us on the device.
+// and entries of rows on pages that were there) instead of nine: a step of 64 sequences 9.4 -> 4.8 us on the device.
 constexpr int kKept = 4096;              // pages of a step that LDS holds; where there are more, they are read back
 struct SharedOnce {
     uint32_t goes[kThreads], takes[kThreads], starts[kThreads + 1];      // of the sequences: where their entries of the flat lists, and their tokens, end
@@ -223,8 +223,8 @@ struct SharedOnce {
     uint32_t taken;
     int32_t back[kKept], fresh[kKept];
 };
-// The first of the ascending sums that lies behind x, or the last of 2 half (half: a power of two, or 0).  (Eight or four searches of a thread at a time, step by step, took LDS longer than
-// they saved in trips to it: a step of 64 sequences 10.4 us for 6.4.)
+// The first of the ascending sums that lies behind x, or the last of 2 half (half: a power of two, or 0).  (For 4096 entries, searches of several at a time, step by step, took LDS longer than they
+// saved in trips to it, 11.9 us for 9.3; marks where sequences begin and a running maximum over them 10.3.)
 __device__ __forceinline__ int first_behind(const uint32_t* sums, int half, uint32_t x)
 {
     int k = 0;
@@ -269,52 +269,72 @@ __global__ __launch_bounds__(kThreads) void paged_reserve_once_kernel(PagePool p
     // Pages that go back.
     const uint32_t base = (uint32_t)min(max(first_free, 0), p.n_pages);
     uint32_t top = base;
-    int turn = 0;
-    for (uint32_t x0 = 0; x0 < all; x0 += kDeep * kThreads, turn ^= 1) {
-        int32_t page[kDeep];
-#pragma unroll
-        for (int i = 0; i < kDeep; ++i) {
-            const uint32_t x = x0 + (uint32_t)(i * kThreads + tid);
-            page[i] = -1;
-            if (x < all) {
-                const int k = first_behind(sm.goes, half, x);
-                int32_t* const entry = p.table + (long long)k * p.table_stride + sm.left[k] + (int)(x - (k ? sm.goes[k - 1] : 0u));
-                page[i] = *entry;
-                *entry = -1;
-            }
+    auto place_of = [&](const uint32_t* sums, int k, uint32_t x) { return p.table + (long long)k * p.table_stride + sm.left[k] + (int)(x - (k ? sums[k - 1] : 0u)); };
+    auto push = [&](unsigned long long in, uint32_t before, int32_t page) {
+        const uint32_t to = top + before + (uint32_t)__popcll(in & ((1ull << lane) - 1ull));
+        if ((in >> lane & 1) && to < (uint32_t)p.n_pages) {      // (more than there are: a page that came twice)
+            stack[to] = page;
+            if (to - base < kKept) sm.back[to - base] = page;
         }
-        unsigned long long in[kDeep];
-#pragma unroll
-        for (int i = 0; i < kDeep; ++i) {
-            in[i] = __ballot((uint32_t)page[i] < (uint32_t)p.n_pages);
-            if (lane == 0) sm.counts[turn][i * kWaves + wave] = (uint32_t)__popcll(in[i]);
+    };
+    if (all <= kThreads) {
+        int32_t page = -1;
+        if ((uint32_t)tid < all) {
+            int32_t* const entry = place_of(sm.goes, first_behind(sm.goes, half, (uint32_t)tid), (uint32_t)tid);
+            page = *entry;
+            *entry = -1;
         }
+        const unsigned long long in = __ballot((uint32_t)page < (uint32_t)p.n_pages);
+        if (lane == 0) sm.counts[0][wave] = (uint32_t)__popcll(in);
         __syncthreads();
-        const uint32_t c0 = sm.counts[turn][2 * lane], c1 = sm.counts[turn][2 * lane + 1];
-        const uint32_t upto = wave_incl_scan_u32(c0 + c1);
+        uint32_t before = 0, sum = 0;
 #pragma unroll
-        for (int i = 0; i < kDeep; ++i) {
-            const int at = i * kWaves + wave;
-            uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(upto - c0 - c1), at >> 1);
-            if (at & 1) before += (uint32_t)__builtin_amdgcn_readlane((int)c0, at >> 1);
-            const uint32_t to = top + before + (uint32_t)__popcll(in[i] & ((1ull << lane) - 1ull));
-            if ((in[i] >> lane & 1) && to < (uint32_t)p.n_pages) {      // (more than there are: a page that came twice)
-                stack[to] = page[i];
-                if (to - base < kKept) sm.back[to - base] = page[i];
-            }
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t n = sm.counts[0][w];
+            before += w < wave ? n : 0u;
+            sum += n;
         }
-        top += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        push(in, before, page);
+        top += sum;
+    } else {
+        int turn = 0;
+        for (uint32_t x0 = 0; x0 < all; x0 += kDeep * kThreads, turn ^= 1) {
+            int32_t page[kDeep];
+            unsigned long long in[kDeep];
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const uint32_t x = x0 + (uint32_t)(i * kThreads + tid);
+                page[i] = -1;
+                if (x < all) {
+                    int32_t* const entry = place_of(sm.goes, first_behind(sm.goes, half, x), x);
+                    page[i] = *entry;
+                    *entry = -1;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                in[i] = __ballot((uint32_t)page[i] < (uint32_t)p.n_pages);
+                if (lane == 0) sm.counts[turn][i * kWaves + wave] = (uint32_t)__popcll(in[i]);
+            }
+            __syncthreads();
+            const uint32_t c0 = sm.counts[turn][2 * lane], c1 = sm.counts[turn][2 * lane + 1];
+            const uint32_t upto = wave_incl_scan_u32(c0 + c1);
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const int at = i * kWaves + wave;
+                uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(upto - c0 - c1), at >> 1);
+                if (at & 1) before += (uint32_t)__builtin_amdgcn_readlane((int)c0, at >> 1);
+                push(in[i], before, page[i]);
+            }
+            top += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        }
     }
     top = min(top, (uint32_t)p.n_pages);
     // Who gets what.
     const bool ok = more == 0 || takes <= top;
     if (!ok) come = 0;
-    unsigned long long upto = (unsigned long long)come;
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) {
-        const unsigned long long v = __shfl_up(upto, step, 64);
-        if (lane >= step) upto += v;
-    }
+    // (halves, so that a wave's sums of each stay within 32 bits)
+    unsigned long long upto = ((unsigned long long)wave_incl_scan_u32((uint32_t)come >> 16) << 16) + wave_incl_scan_u32((uint32_t)come & 0xffffu);
     if (lane == 63) sm.tokens[wave] = upto;
     const unsigned long long got = __ballot(ok && more > 0);
     if (got && lane == 63 - __clzll((long long)got)) atomicMax(&sm.taken, takes);
@@ -335,13 +355,18 @@ __global__ __launch_bounds__(kThreads) void paged_reserve_once_kernel(PagePool p
     const uint32_t taken = sm.taken;
     if (tid == 0) p.n_free[0] = (int32_t)(top - taken);
     if (top - base > kKept) __syncthreads();               // (the stack is read back)
-    for (uint32_t x = tid; x < taken; x += kThreads) {
+    auto popped = [&](uint32_t x) {
         const uint32_t from = top - 1u - x;
-        const int32_t page = from >= base && top - base <= kKept ? sm.back[from - base] : stack[from];
-        const int k = first_behind(sm.takes, half, x);
-        p.table[(long long)k * p.table_stride + sm.left[k] + (int)(x - (k ? sm.takes[k - 1] : 0u))] = page;
-        stack[from] = -1;
+        return from >= base && top - base <= kKept ? sm.back[from - base] : stack[from];
+    };
+    auto take = [&](uint32_t x, int k, int32_t page) {
+        *place_of(sm.takes, k, x) = page;
+        stack[top - 1u - x] = -1;
         if (x < kKept) sm.fresh[x] = page;
+    };
+    for (uint32_t x = tid; x < taken; x += kThreads) {
+        const int32_t page = popped(x);
+        take(x, first_behind(sm.takes, half, x), page);
     }
     if (rows.n_rows <= 0) return;
     __syncthreads();
@@ -372,13 +397,20 @@ __global__ __launch_bounds__(256) void paged_map_kernel(PagePool p, StepRows row
     if (r0 < rows.n_rows) map_rows(p, rows, r0);
 }
 
-constexpr int kMapped = 4096;            // rows that the one workgroup maps itself
+// Whether the one workgroup maps the rows itself: it looks each one's sequence up by a search, as long as there are sequences, and a launch of its own costs 3.6 us whatever it does.  By itself and by
+// a launch, us a call: 6000 rows of 8 sequences 7.4 and 10.3, of 64 8.5 and 10.2, of 200 9.7 and 10.2, of 1000 10.8 and 10.3; 7500 of 1000 12.0 and 10.2.
+bool mapped_along(int n_rows, int n_seqs)
+{
+    int steps = 4;
+    while (steps < 14 && 1 << (steps - 4) < n_seqs) ++steps;
+    return (long long)n_rows * steps <= 1 << 16;
+}
 
 }  // namespace
 
 hipError_t launch_paged_reserve(const PagePool& p, const int32_t* n_new, const int32_t* keep, int32_t* granted, const StepRows& rows, hipStream_t s)
 {
-    const bool apart = rows.n_rows > kMapped;
+    const bool apart = !mapped_along(rows.n_rows, p.n_seqs);
     StepRows here = rows;
     if (apart) here.n_rows = 0;
     const auto on = p.n_seqs <= kThreads ? Launch<paged_reserve_once_kernel>::on : Launch<paged_reserve_kernel>::on;

@@ -22,7 +22,7 @@ __device__ __forceinline__ void lds_read(u32x4 (&w)[2], uint32_t at)
 }
 __device__ __forceinline__ void lds_read(u32x4 (&w)[4], uint32_t at)
 {
-    asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %4 offset:3072\n\ts_waitcnt lgkmcnt(0)"
+    asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:0x400\n\tds_read_b128 %2, %4 offset:0x800\n\tds_read_b128 %3, %4 offset:0xc00\n\ts_waitcnt lgkmcnt(0)"
                  : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3])
                  : "v"(at)
                  : "memory");
