@@ -285,6 +285,8 @@ class MpRotary:
 
     def mp_norm_rotary(self, norm, x, positions=None, out=None, lookup_position=None, out_lookup=None):
         """mp_rotary of rows that are normed first (norm: MpHeadNorm), in the same pass."""
+        if norm is None:
+            _reject("the norm is missing")
         return self._turn(norm, x, positions, out, lookup_position, out_lookup)
 
     def _turn(self, norm, x, positions, out, lookup_position, out_lookup):
@@ -392,6 +394,8 @@ class MpPagedKv:
 
     def mp_paged_tree_attention(self, q, mask, max_new=0, window=0, softmax_scale=0.0, out=None, lse=None, workspace=None):
         """mp_paged_attention of a tree's tokens: each attends its sequence's older keys and the new ones that its mask (int64 [tokens, words]) marks."""
+        if mask is None:
+            _reject("the mask is missing")
         return self._attend(q, mask, max_new, window, softmax_scale, out, lse, workspace)
 
     def _attend(self, q, mask, max_new, window, softmax_scale, out, lse, workspace):

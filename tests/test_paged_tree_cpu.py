@@ -114,3 +114,10 @@ def test_trees_refuse(mp):
     _refused(mp, attend(size=5), "workspace")
     _refused(mp, attend(ws=None), "workspace")
     assert plan(T=0) == mp.MP_OK and plan(_cache(mp, n_seqs=0)) == mp.MP_OK and keep(_cache(mp, n_seqs=0)) == mp.MP_OK and attend(T=0) == mp.MP_OK
+
+
+def test_a_missing_mask_or_norm_is_not_the_plain_call(mp):
+    for call in (lambda: object.__new__(mp.MpPagedKv).mp_paged_tree_attention(None, None), lambda: object.__new__(mp.MpRotary).mp_norm_rotary(None, None)):
+        with pytest.raises(mp.MpError, match="is missing") as e:
+            call()
+        assert e.value.status == mp.MP_EINVAL
