@@ -47,6 +47,9 @@ MP_PAGE_FN void blocks_of(int base, int i0, int i1, int window, int room, int un
 // The lowest n of 64 bits.
 MP_PAGE_FN unsigned long long below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 
+// The parent of a tree's token: the number that the caller gave, if it is that of a token before it, or -1 (which, unlike any other number below zero, stays what it is in 16 bits).
+MP_PAGE_FN int parent_of(int given, int token) { return given >= 0 && given < token ? given : -1; }
+
 // A row of a tree attends the keys of its sequence that are older than the `n` new ones, `base` of them, and the new ones that its mask marks (bit i % 64 of word i / 64: the i-th); a window
 // leaves it the last ones of all these.  Either way it attends the keys from a first one on, `low`, that are older or marked.
 MP_PAGE_FN int tree_low(const unsigned long long* mask, int words, int base, int n, int window)

@@ -34,8 +34,7 @@ __global__ __launch_bounds__(64 * kWords) void paged_tree_plan_kernel(PagedKv c,
     __shared__ int16_t up[kTokens];
     const int b = blockIdx.x, i = threadIdx.x;
     const NewTokens t = new_tokens(c, n_tokens, b, 64 * words);
-    int ancestor = i < t.n ? parents[t.q0 + i] : -1;
-    if (ancestor >= i) ancestor = -1;
+    int ancestor = i < t.n ? parent_of(parents[t.q0 + i], i) : -1;
     unsigned long long own[kWords];
 #pragma unroll
     for (int w = 0; w < kWords; ++w) own[w] = w == i >> 6 ? 1ull << (i & 63) : 0ull;
