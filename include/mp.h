@@ -560,7 +560,8 @@ typedef struct {
  * [0, n_pages) have no page to give).  Then each sequence, in order, takes pages for its keys that stay and its tokens from the stack's top.  Where these are too few, that
  * sequence and all behind it that need a page get no tokens (a sequence whose last page has room for its tokens gets them); nor does one whose table has no room.
  * Places of the stack that were taken become -1.  Then kv_len = keep + granted, and q_start is the running sum of granted.
- * The same arrays in give the same ones out.  n_new and keep are not results of the same call.  Errors: MP_EINVAL, MP_EHIP. */
+ * The same arrays in give the same ones out.  n_new and keep are not results of the same call.  Errors: MP_EINVAL (also for n_rows past 2^31 - 65, or n_seqs past
+ * 2^31 - 1025), MP_EHIP. */
 mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const int32_t* keep, int32_t* granted, int32_t* sequence,
                            int32_t* positions, int64_t* slots, int32_t n_rows, void* stream);
 

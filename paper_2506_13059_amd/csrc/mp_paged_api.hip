@@ -359,6 +359,8 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
     }
     if (n_rows < 0) return fail(nullptr, MP_EINVAL, "%s: n_rows %d < 0", who, n_rows);
     if (!sequence && !positions && !slots) n_rows = 0;
+    // (sequences are gone through 1024 and rows 64 at a time, in 32 bits; a row of 2^31 - 1 would lie before no start)
+    if (n_rows > kMostKeys - 64 || pool->n_seqs > kMostKeys - 1024) return fail(nullptr, MP_EINVAL, "%s: too many rows or sequences", who);
     if ((uintptr_t)slots & 7) return fail(nullptr, MP_EINVAL, "%s: slots do not start on 8 bytes", who);
     PagePool p;
     p.table = pool->page_table;
