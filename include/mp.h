@@ -560,7 +560,7 @@ typedef struct {
  * [0, n_pages) have no page to give).  Then each sequence, in order, takes pages for its keys that stay and its tokens from the stack's top.  Where these are too few, that
  * sequence and all behind it that need a page get no tokens (a sequence whose last page has room for its tokens gets them); nor does one whose table has no room.
  * Places of the stack that were taken become -1.  Then kv_len = keep + granted, and q_start is the running sum of granted.
- * The same arrays in give the same ones out.  n_new and keep are not results of the same call.  Errors: MP_EINVAL (also for n_rows past 2^31 - 65, or n_seqs past
+ * The same arrays in give the same ones out.  What is written overlaps no other argument, nor do n_new and keep lie in it.  Errors: MP_EINVAL (also for n_rows past 2^31 - 65, or n_seqs past
  * 2^31 - 1025), MP_EHIP. */
 mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const int32_t* keep, int32_t* granted, int32_t* sequence,
                            int32_t* positions, int64_t* slots, int32_t n_rows, void* stream);
@@ -573,7 +573,8 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
  *   parents     device int32 [n_tokens]: the parent's number among the new tokens of its sequence; anything that is no token before it: none
  *   mask        device uint64 [n_tokens, mask_words]: the token and its ancestors
  *   positions   device int32 [n_tokens]: kv_len - n + (ancestors), with n new tokens: what mp_paged_append_norm turns a token to
- * Of a sequence, the first 64 * mask_words new tokens have results; other rows are left as they were.  The pages are not looked at.  Errors: MP_EINVAL, MP_EHIP.
+ * Of a sequence, the first 64 * mask_words new tokens have results; other rows are left as they were.  The pages are not looked at.  Errors: MP_EINVAL (also where a result overlaps what is
+ * read), MP_EHIP.
  *
  * mp_paged_tree_attention -- every new token attends the keys of its sequence that are older than the new ones, and the new ones that its mask marks (any, also
  * such as stand behind it; itself only if it is marked).  window: of all these, the last `window` keys (marks, whether or not their pages are
@@ -585,7 +586,7 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
  *   mask        as above, [n_tokens, mask_words]
  *   leaf        device int32 [n_seqs], the last accepted one among the new tokens of its sequence; anything else (or one that has no mask): none is accepted
  *   keep        device int32 [n_seqs]: kv_len - n + (marked tokens), what mp_paged_reserve keeps in the next step; kv_len and q_start stay as they are
- * One call a layer's pages.  Errors: MP_EINVAL, MP_EHIP. */
+ * One call a layer's pages.  Errors: MP_EINVAL (also where keep overlaps what is read), MP_EHIP. */
 mp_status mp_paged_tree_plan(const mp_paged_kv* cache, const int32_t* parents, int32_t n_tokens, int32_t mask_words, uint64_t* mask,
                              int32_t* positions, void* stream);
 mp_status mp_paged_tree_attention(const mp_paged_kv* cache, const void* q, int64_t q_stride, const uint64_t* mask, int32_t mask_words,

@@ -97,6 +97,30 @@ mp_status cache_ok(const char* who, const mp_paged_kv* c, PagedKv* out)
     return MP_OK;
 }
 
+// `count` of `bytes` each; a null pointer overlaps nothing.
+struct Span {
+    const void* p;
+    long long count;
+    int bytes;
+};
+bool overlap(const Span& a, const Span& b)
+{
+    const uintptr_t a0 = (uintptr_t)a.p, a1 = a0 + (uintptr_t)(a.count * a.bytes), b0 = (uintptr_t)b.p, b1 = b0 + (uintptr_t)(b.count * b.bytes);
+    return a.p && b.p && a0 < b1 && b0 < a1;
+}
+// Whether a result lies on something that is read, or on another result.
+template <int kResults, int kRead>
+bool overlap(const Span (&results)[kResults], const Span (&read)[kRead])
+{
+    for (int i = 0; i < kResults; ++i) {
+        for (const Span& r : read)
+            if (overlap(results[i], r)) return true;
+        for (int j = 0; j < i; ++j)
+            if (overlap(results[i], results[j])) return true;
+    }
+    return false;
+}
+
 mp_status launched(const char* who, hipError_t e)
 {
     return e == hipSuccess ? MP_OK : fail(nullptr, MP_EHIP, "%s: %s", who, hipGetErrorString(e));
@@ -306,6 +330,9 @@ mp_status mp_paged_tree_attention(const mp_paged_kv* cache, const void* q, int64
     PagedTreeAttention a{};
     const mp_status st = mask_ok(who, mask, mask_words, n_tokens);
     if (st != MP_OK) return st;
+    const long long rows = (long long)n_tokens * n_q_heads, marks = (long long)n_tokens * mask_words;
+    if (overlap(Span{out, rows, 2 * kHeadDimHost}, Span{mask, marks, 8}) || overlap(Span{lse, rows, 4}, Span{mask, marks, 8}))
+        return fail(nullptr, MP_EINVAL, "%s: out or lse overlaps the mask", who);
     a.mask = (const unsigned long long*)mask;
     a.words = mask_words;
     return attention(who, a, cache, q, q_stride, n_tokens, n_q_heads, max_new, window, softmax_scale, out, lse, workspace, workspace_bytes, stream);
@@ -319,8 +346,10 @@ mp_status mp_paged_tree_plan(const mp_paged_kv* cache, const int32_t* parents, i
     if (st != MP_OK || (st = mask_ok(who, mask, mask_words, n_tokens)) != MP_OK) return st;
     if (n_tokens == 0 || c.n_seqs == 0) return MP_OK;
     if (!parents || !positions) return fail(nullptr, MP_EINVAL, "%s: null parents or positions", who);
-    if (parents == positions) return fail(nullptr, MP_EINVAL, "%s: positions overlap the parents", who);
     if (c.n_seqs > kMostSequences) return fail(nullptr, MP_EINVAL, "%s: more than %d sequences", who, kMostSequences);
+    // (other sequences' workgroups read while one writes)
+    if (overlap({{mask, (long long)n_tokens * mask_words, 8}, {positions, n_tokens, 4}}, {{parents, n_tokens, 4}, {c.kv_len, c.n_seqs, 4}, {c.q_start, c.n_seqs + 1ll, 4}}))
+        return fail(nullptr, MP_EINVAL, "%s: the mask or the positions overlap another argument", who);
     return launched(who, launch_paged_tree_plan(c, parents, n_tokens, mask_words, mask, positions, (hipStream_t)stream));
 }
 
@@ -332,8 +361,10 @@ mp_status mp_paged_tree_keep(const mp_paged_kv* cache, const uint64_t* mask, int
     if (st != MP_OK || (st = mask_ok(who, mask, mask_words, n_tokens)) != MP_OK) return st;
     if (c.n_seqs == 0) return MP_OK;
     if (!leaf || !keep) return fail(nullptr, MP_EINVAL, "%s: null leaf or keep", who);
-    if (keep == c.kv_len || keep == leaf) return fail(nullptr, MP_EINVAL, "%s: keep overlaps another argument", who);
     if (2ll * c.n_kv * c.n_seqs > kMostTokens) return fail(nullptr, MP_EINVAL, "%s: too many heads of sequences", who);
+    if (overlap({{keep, c.n_seqs, 4}}, {{leaf, c.n_seqs, 4}, {mask, (long long)n_tokens * mask_words, 8}, {c.kv_len, c.n_seqs, 4}, {c.q_start, c.n_seqs + 1ll, 4},
+                                        {c.table, (long long)c.n_seqs * c.table_stride, 4}}))
+        return fail(nullptr, MP_EINVAL, "%s: keep overlaps another argument", who);
     return launched(who, launch_paged_tree_keep(c, mask, mask_words, leaf, n_tokens, keep, (hipStream_t)stream));
 }
 
@@ -351,16 +382,15 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
     if ((long long)pool->n_seqs * pool->table_stride > kMostKeys) return fail(nullptr, MP_EINVAL, "%s: the page table has more than 2^31 - 1 entries", who);
     if (!pool->free_pages || !pool->n_free || !pool->q_start) return fail(nullptr, MP_EINVAL, "%s: null free_pages, n_free or q_start", who);
     if (pool->n_seqs > 0 && (!pool->page_table || !pool->kv_len || !n_new)) return fail(nullptr, MP_EINVAL, "%s: null page_table, kv_len or n_new", who);
-    const void* outs[] = {pool->page_table, pool->kv_len, pool->q_start, pool->free_pages, pool->n_free, granted, sequence, positions, slots};
-    for (int i = 0; i < 9; ++i) {
-        if (outs[i] && (outs[i] == n_new || outs[i] == keep)) return fail(nullptr, MP_EINVAL, "%s: n_new or keep overlaps what is written", who);
-        for (int j = 0; j < i; ++j)
-            if (outs[i] && outs[i] == outs[j]) return fail(nullptr, MP_EINVAL, "%s: two results overlap", who);
-    }
     if (n_rows < 0) return fail(nullptr, MP_EINVAL, "%s: n_rows %d < 0", who, n_rows);
     if (!sequence && !positions && !slots) n_rows = 0;
     // (sequences are gone through 1024 and rows 64 at a time, in 32 bits; a row of 2^31 - 1 would lie before no start)
     if (n_rows > kMostKeys - 64 || pool->n_seqs > kMostKeys - 1024) return fail(nullptr, MP_EINVAL, "%s: too many rows or sequences", who);
+    const long long n = pool->n_seqs;
+    if (overlap({{pool->page_table, n * pool->table_stride, 4}, {pool->kv_len, n, 4}, {pool->q_start, n + 1, 4}, {pool->free_pages, pool->n_pages, 4}, {pool->n_free, 1, 4},
+                 {granted, n, 4}, {sequence, n_rows, 4}, {positions, n_rows, 4}, {slots, n_rows, 8}},
+                {{n_new, n, 4}, {keep, n, 4}}))
+        return fail(nullptr, MP_EINVAL, "%s: what is written overlaps another argument", who);
     if ((uintptr_t)slots & 7) return fail(nullptr, MP_EINVAL, "%s: slots do not start on 8 bytes", who);
     PagePool p;
     p.table = pool->page_table;
