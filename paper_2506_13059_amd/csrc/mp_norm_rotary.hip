@@ -32,6 +32,17 @@ __device__ __forceinline__ float row_factor(const float (&x)[8], float eps)
     return rsqrtf(fmaf(row_sum_f32(s), 1.f / kHeadDim, eps));
 }
 
+// The partners of the dims that are turned; for the others, themselves: what they meet is a sine of zero, and an infinity of a neighbour would make NaN of it.
+__device__ __forceinline__ void turned_partners(const uint4& w, const Turn& t, const Rotation& rot, float (&y)[8])
+{
+    partners(w, t, rot, y);
+    if (!rot.interleaved || rot.rot_dim == kHeadDim) return;
+    float x[8];
+    unpack(w, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = i < t.n ? y[i] : x[i];
+}
+
 // The weights of a lane's dims and of their partners, with the offset.
 struct Weights {
     float own[8], partner[8];
@@ -40,7 +51,7 @@ __device__ __forceinline__ Weights weights_of(const uint4& w, float offset, cons
 {
     Weights r;
     unpack(w, r.own);
-    partners(w, t, rot, r.partner);
+    turned_partners(w, t, rot, r.partner);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         r.own[i] += offset;
@@ -104,7 +115,7 @@ __device__ __forceinline__ void normed_rows(const Rows& r, const HeadNorm& norm,
             if (h0 + 4 * i >= r.h1) break;
             float x[8], y[8];
             unpack(v[i], x);
-            partners(v[i], first, rot, y);
+            turned_partners(v[i], first, rot, y);
             const float f = row_factor(x, norm.eps);
             if constexpr (kHeads) {
                 const Weights u = weights_of(w[i], norm.offset, first, rot);
