@@ -440,8 +440,7 @@ mp_status mp_rotary(const mp_rotary_spec* rotary, const void* x, int64_t x_strid
                     int32_t lookup_position, void* stream);
 
 /* Norm of a head's rows: x / sqrt(mean(x^2) + eps) * (weight + offset), the mean over the row's 128 elements.  Worked out in fp32 with what follows it, and rounded to bf16 once.
- * A row whose squares' sum passes fp32 (elements from 1.6e18 on) may be zero; one with an infinity is NaN in that element and its partner of the rotation, and zero elsewhere; one with a NaN
- * is NaN. */
+ * A row with an infinity is NaN in that element and its partner of the rotation, if it is turned, and zero elsewhere; one with a NaN is NaN. */
 typedef struct {
     const void* weight;    /* device bf16 [n_heads, 128]                                              */
     int32_t n_heads;       /* heads of the rows, or 1: the same weights for all of them               */
