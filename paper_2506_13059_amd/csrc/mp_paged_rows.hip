@@ -48,13 +48,28 @@ __device__ __forceinline__ void workgroup_sync()
     asm volatile("" ::: "memory");
 }
 
-// kOnePage: a page holds the rows that a wave brings of a block, so that their address is a scalar.
+// Four bytes a lane, lane i's to lds_off + 4 i.
+__device__ __forceinline__ void load4_to_lds(const void* src, uint32_t lds_off)
+{
+    auto* dst = reinterpret_cast<__attribute__((address_space(3))) uint32_t*>((uintptr_t)lds_off);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src, dst, 4, 0, 0);
+}
+__device__ __forceinline__ int lds_read4(uint32_t at)
+{
+    int w;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(at) : "memory");
+    return w;
+}
+
+// kOnePage: a page holds the rows that a wave brings of a block, so that their address is a scalar.  Entries of smaller pages go to LDS as the rows do, two blocks before they are used: a load to
+// a register is waited for with all that was asked for before it, which were the three blocks on their way.  12 tokens each of 8 sequences of up to 30K, 8 KV heads of four, pages of 8: 97.2 us
+// and, so, 90.9 (pages of 16 rows 87.9); pages of one 102.7 and 93.3; 24 each, pages of 4, where it is eight waves' instructions that take the time, 107.0 and 108.4.
 template <int kWaves, bool kOnePage>
 __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kernel(PagedTreeAttention a, Tiling tl, float* parts, Cut* cuts)
 {
     constexpr int kBring = kKeys / kWaves, kLoads = kBring / 4;          // rows that a wave brings of a block, and instructions for its keys
     constexpr int kBitBytes = kBring / 8;
-    __shared__ __align__(256) unsigned char lds[kRing * kBlockBytes + 2 * kRing * 8];
+    __shared__ __align__(256) unsigned char lds[kRing * kBlockBytes + 2 * kRing * 8 + (kOnePage ? 0 : kWaves * kRing * 256)];
     const uint32_t ring = (uint32_t)(uintptr_t)(lds_byte*)lds, valid_at = ring + kRing * kBlockBytes, odd_at = valid_at + kRing * 8;      // (a bit a key: there; its values not all finite)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const float top = hidden_infinity();
@@ -72,7 +87,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
     const int vr = 4 * g + (col >> 2);
     const uint32_t v_at = ring + kValues + (uint32_t)(vr * 256 + ((((col & 3) >> 1) ^ ((vr & 7) << 1)) << 4) + (col & 1) * 8);      // ^ 32 d
     const int row0 = kBring * wave;
-    const uint32_t wave_at = ring + (uint32_t)((row0 >> 5) * kHalf + (row0 & 31) * 256);
+    const uint32_t wave_at = ring + (uint32_t)((row0 >> 5) * kHalf + (row0 & 31) * 256), entries_at = odd_at + kRing * 8 + (uint32_t)(wave * kRing * 256);
     uint32_t k_from[kLoads], v_from[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -97,11 +112,14 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
         const int32_t* entries = a.c.table + (long long)it.b * a.c.table_stride;
         typedef const __attribute__((address_space(4))) int32_t constant_int;
         // What a wave needs to know of them: the entry (or, for small pages, one of each row in lanes 64 / kBring r ..).
+        auto place_at = [&](int block) { return max(min(block * kKeys + row0 + (kOnePage ? 0 : lane / (64 / kBring)), end - 1), 0) >> a.c.page_shift; };
         auto entry_at = [&](int block) {
-            const int key = block * kKeys + row0;
-            if constexpr (kOnePage) return (int)((constant_int*)entries)[max(min(key, end - 1), 0) >> a.c.page_shift];
-            else return (int)entries[max(min(key + lane / (64 / kBring), end - 1), 0) >> a.c.page_shift];
+            if constexpr (kOnePage) return (int)((constant_int*)entries)[place_at(block)];
+            else return (int)entries[place_at(block)];
         };
+        // (small pages: asked for, and read by the same wave when blocks behind have come)
+        auto ask = [&](int block) { load4_to_lds(entries + place_at(block), entries_at + (uint32_t)((block & (kRing - 1)) * 256)); };
+        auto asked = [&](int block) { return lds_read4(entries_at + (uint32_t)((block & (kRing - 1)) * 256 + lane * 4)); };
         // A bit for each of them that is there.
         auto bits_of = [&](int block, int entry) {
             const int n = end - (block * kKeys + row0);
@@ -135,10 +153,11 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
                 }
             }
         };
-        int entry[4];
+        constexpr int kEntries = kOnePage ? 4 : 3;
+        int entry[kEntries];
         uint32_t bits[4];                                  // of blocks t .. t + 3
 #pragma unroll
-        for (int i = 0; i < 4; ++i) entry[i] = entry_at(min(first + i, last - 1));
+        for (int i = 0; i < kEntries; ++i) entry[i] = entry_at(min(first + i, last - 1));
 
         // this lane's query row
         const int tile_rows = min(it.rows.n - it.tile * tl.tokens, tl.tokens) * G;
@@ -211,12 +230,16 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
         for (int d = 0; d < 8; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (end > 0) {
             workgroup_sync();                              // (the item before is done with LDS)
+            if constexpr (!kOnePage) {
+                ask(min(first + 3, last - 1));
+                ask(min(first + 4, last - 1));
+            }
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
                 bits[i] = bits_of(min(first + i, last - 1), entry[i]);
                 if (first + i < last) load(first + i, entry[i], bits[i]);
             }
-            int next = entry[3];
+            int next = entry[kEntries - 1];
             wait_for(first);
             arrived(first, bits[0]);
             workgroup_sync();
@@ -224,9 +247,13 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
                 const int place = t & (kRing - 1);
                 const uint32_t slot = (uint32_t)(place * kBlockBytes);
                 if (t + 3 < last) {                        // (its place was that of t - 1, which all waves are done with)
+                    if constexpr (!kOnePage) {
+                        ask(min(t + 5, last - 1));
+                        next = asked(t + 3);
+                    }
                     bits[3] = bits_of(t + 3, next);
                     load(t + 3, next, bits[3]);
-                    next = entry_at(min(t + 4, last - 1));
+                    if constexpr (kOnePage) next = entry_at(min(t + 4, last - 1));
                 }
                 if (active) {
                     f32x4 s[4];
