@@ -572,6 +572,7 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
  *   parents     device int32 [n_tokens]: the parent's number among the new tokens of its sequence; anything that is no token before it: none
  *   mask        device uint64 [n_tokens, mask_words]: the token and its ancestors
  *   positions   device int32 [n_tokens]: kv_len - n + (ancestors), with n new tokens: what mp_paged_append_norm turns a token to
+ *   mask_words  or'ed with MP_TREE_EVERY_ROW: rows without a result get a mask of zeros (older keys alone) and position -1
  * Of a sequence, the first 64 * mask_words new tokens have results; other rows are left as they were.  The pages are not looked at.  Errors: MP_EINVAL (also where a result overlaps what is
  * read), MP_EHIP.
  *
@@ -586,6 +587,7 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
  *   leaf        device int32 [n_seqs], the last accepted one among the new tokens of its sequence; anything else (or one that has no mask): none is accepted
  *   keep        device int32 [n_seqs]: kv_len - n + (marked tokens), what mp_paged_reserve keeps in the next step; kv_len and q_start stay as they are
  * One call a layer's pages.  Errors: MP_EINVAL (also where keep overlaps what is read), MP_EHIP. */
+#define MP_TREE_EVERY_ROW 256
 mp_status mp_paged_tree_plan(const mp_paged_kv* cache, const int32_t* parents, int32_t n_tokens, int32_t mask_words, uint64_t* mask,
                              int32_t* positions, void* stream);
 mp_status mp_paged_tree_attention(const mp_paged_kv* cache, const void* q, int64_t q_stride, const uint64_t* mask, int32_t mask_words,

@@ -30,6 +30,7 @@ EXPORTS = [
 MP_KV_BF16, MP_KV_E4M3 = 0, 1
 MP_ROTARY_HALF, MP_ROTARY_INTERLEAVED = 0, 1
 MP_ROTARY_PLAIN, MP_ROTARY_LINEAR, MP_ROTARY_BASE, MP_ROTARY_BY_PARTS = range(4)
+MP_TREE_EVERY_ROW = 256
 
 
 class MpError(RuntimeError):
@@ -416,15 +417,21 @@ class MpPagedKv:
 
     def mp_paged_tree_plan(self, parents, mask_words=1, mask=None, positions=None):
         """parents int32 [tokens], numbers within a sequence's new tokens (no token before it: none) -> (mask int64 [tokens, mask_words] of each token and its
-        ancestors, positions int32 [tokens]).  Rows of no sequence are left as they were: where that matters, pass tensors."""
+        ancestors, positions int32 [tokens]).  Tokens of a sequence from 64 * mask_words on, and rows of no sequence, have no result: a mask of zeros and position -1
+        in tensors that are made here; in tensors that are passed, such rows are left as they were."""
         device = self._current()
         n = parents.shape[0] if parents.dim() == 1 else -1
         _dense(parents, "parents", torch.int32, (n,), device)
-        if mask_words < 1:
-            _reject(f"mask_words = {mask_words} < 1")
-        mask = parents.new_empty(n, mask_words, dtype=torch.int64) if mask is None else _dense(mask, "mask", torch.int64, (n, mask_words), device)
-        positions = torch.empty_like(parents) if positions is None else _dense(positions, "positions", torch.int32, (n,), device)
-        st = lib().mp_paged_tree_plan(self.at, parents.data_ptr(), n, mask_words, mask.data_ptr(), positions.data_ptr(), _stream_of(device))
+        if not 1 <= mask_words <= 16:
+            _reject(f"mask_words = {mask_words} is not 1 .. 16")
+        words = mask_words
+        if mask is None and positions is None:
+            words |= MP_TREE_EVERY_ROW
+            mask, positions = parents.new_empty(n, mask_words, dtype=torch.int64), torch.empty_like(parents)
+        else:
+            mask = parents.new_zeros((n, mask_words), dtype=torch.int64) if mask is None else _dense(mask, "mask", torch.int64, (n, mask_words), device)
+            positions = torch.full_like(parents, -1) if positions is None else _dense(positions, "positions", torch.int32, (n,), device)
+        st = lib().mp_paged_tree_plan(self.at, parents.data_ptr(), n, words, mask.data_ptr(), positions.data_ptr(), _stream_of(device))
         if st:
             _check(st)
         return mask, positions

@@ -62,7 +62,8 @@ struct StepRows {
 hipError_t launch_paged_reserve(const PagePool& p, const int32_t* n_new, const int32_t* keep, int32_t* granted, const StepRows& rows, hipStream_t s);
 
 // Trees of drafted tokens: every token's mask of `words` 64-bit words marks tokens of its sequence.
-hipError_t launch_paged_tree_plan(const PagedKv& c, const int32_t* parents, int n_tokens, int words, uint64_t* mask, int32_t* positions, hipStream_t s);
+// every: rows without a result get a mask of zeros and position -1.
+hipError_t launch_paged_tree_plan(const PagedKv& c, const int32_t* parents, int n_tokens, int words, bool every, uint64_t* mask, int32_t* positions, hipStream_t s);
 hipError_t launch_paged_tree_keep(const PagedKv& c, const uint64_t* mask, int words, const int32_t* leaf, int n_tokens, int32_t* keep, hipStream_t s);
 
 struct PagedAttention {

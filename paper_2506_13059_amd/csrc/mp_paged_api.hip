@@ -343,14 +343,16 @@ mp_status mp_paged_tree_plan(const mp_paged_kv* cache, const int32_t* parents, i
     const char* who = "mp_paged_tree_plan";
     PagedKv c;
     mp_status st = cache_ok(who, cache, &c);
+    const bool every = mask_words > 0 && (mask_words & MP_TREE_EVERY_ROW);
+    if (every) mask_words &= ~MP_TREE_EVERY_ROW;
     if (st != MP_OK || (st = mask_ok(who, mask, mask_words, n_tokens)) != MP_OK) return st;
-    if (n_tokens == 0 || c.n_seqs == 0) return MP_OK;
+    if (n_tokens == 0 || (c.n_seqs == 0 && !every)) return MP_OK;
     if (!parents || !positions) return fail(nullptr, MP_EINVAL, "%s: null parents or positions", who);
     if (c.n_seqs > kMostSequences) return fail(nullptr, MP_EINVAL, "%s: more than %d sequences", who, kMostSequences);
     // (other sequences' workgroups read while one writes)
     if (overlap({{mask, (long long)n_tokens * mask_words, 8}, {positions, n_tokens, 4}}, {{parents, n_tokens, 4}, {c.kv_len, c.n_seqs, 4}, {c.q_start, c.n_seqs + 1ll, 4}}))
         return fail(nullptr, MP_EINVAL, "%s: the mask or the positions overlap another argument", who);
-    return launched(who, launch_paged_tree_plan(c, parents, n_tokens, mask_words, mask, positions, (hipStream_t)stream));
+    return launched(who, launch_paged_tree_plan(c, parents, n_tokens, mask_words, every, mask, positions, (hipStream_t)stream));
 }
 
 mp_status mp_paged_tree_keep(const mp_paged_kv* cache, const uint64_t* mask, int32_t mask_words, int32_t n_tokens, const int32_t* leaf, int32_t* keep, void* stream)

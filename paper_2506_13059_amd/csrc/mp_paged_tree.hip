@@ -24,16 +24,18 @@ __device__ __forceinline__ NewTokens new_tokens(const PagedKv& c, int n_tokens, 
 }
 
 // One workgroup a sequence, one thread a token.  Masks double the length of path that they hold from round to round, until every path has ended: as many rounds as the
-// depth has binary digits.
+// depth has binary digits.  every: rows without a result, a sequence's own and, for the first and the last one, those of no sequence, get a mask of zeros and position -1.
 template <int kWords>
-__global__ __launch_bounds__(64 * kWords) void paged_tree_plan_kernel(PagedKv c, const int32_t* parents, int n_tokens, int words, unsigned long long* mask,
-                                                                      int32_t* positions)
+__global__ __launch_bounds__(64 * kWords) void paged_tree_plan_kernel(PagedKv c, const int32_t* parents, int n_tokens, int words, bool every,
+                                                                      unsigned long long* mask, int32_t* positions)
 {
     constexpr int kTokens = 64 * kWords;
     __shared__ unsigned long long masks[kTokens * kWords];
     __shared__ int16_t up[kTokens];
     const int b = blockIdx.x, i = threadIdx.x;
-    const NewTokens t = new_tokens(c, n_tokens, b, 64 * words);
+    NewTokens t = b < c.n_seqs ? new_tokens(c, n_tokens, b, 0x7fffffff) : NewTokens{};
+    const int rest = b < c.n_seqs - 1 ? t.q0 + t.n : n_tokens;      // behind the last row that is the workgroup's to look after
+    t.n = min(t.n, 64 * words);
     int ancestor = i < t.n ? parent_of(parents[t.q0 + i], i) : -1;
     unsigned long long own[kWords];
 #pragma unroll
@@ -49,14 +51,23 @@ __global__ __launch_bounds__(64 * kWords) void paged_tree_plan_kernel(PagedKv c,
             ancestor = up[ancestor];
         }
     }
-    if (i >= t.n) return;
-    int depth = 0;
+    if (i < t.n) {
+        int depth = 0;
 #pragma unroll
-    for (int w = 0; w < kWords; ++w) {
-        depth += __popcll(own[w]);
-        if (w < words) mask[(long long)(t.q0 + i) * words + w] = own[w];
+        for (int w = 0; w < kWords; ++w) {
+            depth += __popcll(own[w]);
+            if (w < words) mask[(long long)(t.q0 + i) * words + w] = own[w];
+        }
+        positions[t.q0 + i] = t.base + depth - 1;
     }
-    positions[t.q0 + i] = t.base + depth - 1;
+    if (!every) return;
+    auto none = [&](long long row) {
+        for (int w = 0; w < words; ++w) mask[row * words + w] = 0;
+        positions[row] = -1;
+    };
+    for (long long row = t.q0 + t.n + i; row < rest; row += kTokens) none(row);
+    if (b == 0)
+        for (long long row = i; row < t.q0; row += kTokens) none(row);
 }
 
 constexpr int kWaves = 4, kDeep = 4, kMostWords = 16;
@@ -107,14 +118,14 @@ __global__ __launch_bounds__(64 * kWaves) void paged_tree_keep_kernel(PagedKv c,
 
 }  // namespace
 
-hipError_t launch_paged_tree_plan(const PagedKv& c, const int32_t* parents, int n_tokens, int words, uint64_t* mask, int32_t* positions, hipStream_t s)
+hipError_t launch_paged_tree_plan(const PagedKv& c, const int32_t* parents, int n_tokens, int words, bool every, uint64_t* mask, int32_t* positions, hipStream_t s)
 {
-    if (n_tokens <= 0 || c.n_seqs <= 0) return hipSuccess;
+    if (n_tokens <= 0 || (c.n_seqs <= 0 && !every)) return hipSuccess;
     int size = 1;
     while (size < words) size *= 2;
     const auto on = size == 1 ? Launch<paged_tree_plan_kernel<1>>::on : size == 2 ? Launch<paged_tree_plan_kernel<2>>::on : size == 4 ? Launch<paged_tree_plan_kernel<4>>::on
                   : size == 8 ? Launch<paged_tree_plan_kernel<8>>::on : Launch<paged_tree_plan_kernel<16>>::on;
-    return on(dim3((unsigned)c.n_seqs), dim3(64 * size), s, c, parents, n_tokens, words, (unsigned long long*)mask, positions);
+    return on(dim3((unsigned)(c.n_seqs > 0 ? c.n_seqs : 1)), dim3(64 * size), s, c, parents, n_tokens, words, every, (unsigned long long*)mask, positions);
 }
 
 hipError_t launch_paged_tree_keep(const PagedKv& c, const uint64_t* mask, int words, const int32_t* leaf, int n_tokens, int32_t* keep, hipStream_t s)
