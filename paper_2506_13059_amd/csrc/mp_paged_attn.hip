@@ -69,9 +69,12 @@ static hipError_t launch_rows(const PagedTreeAttention& a, hipStream_t s, bool* 
 {
     const long long rows = (long long)a.max_new * (a.n_q_heads / a.c.n_kv);
     const int most = rows <= 64 ? 64 : 128;
-    // (the workspace is that of paged_partial_floats, whichever kernel runs: of 33 rows on, it holds the parts of 64, and of 65 on more than those of 128)
-    *done = rows > 32 && rows <= 128 && paged_token_floats(most) <= paged_partial_floats(a.n_tokens, a.n_q_heads, a.c.n_kv, a.c.n_seqs, a.max_new);
-    return *done ? launch_paged_tree_rows(a, most, a.partials, s) : hipSuccess;
+    *done = rows > 32 && rows <= 128;
+    if (!*done) return hipSuccess;
+    // (the workspace is that of paged_partial_floats, whichever kernel runs: of 33 rows on, it holds the parts of 64, and of 65 on more than those of 128.  No part is written past it, should a
+    // rule there change)
+    if (paged_token_floats(most) > paged_partial_floats(a.n_tokens, a.n_q_heads, a.c.n_kv, a.c.n_seqs, a.max_new)) return hipErrorInvalidValue;
+    return launch_paged_tree_rows(a, most, a.partials, s);
 }
 static hipError_t launch_rows(const PagedAttention&, hipStream_t, bool* done)
 {

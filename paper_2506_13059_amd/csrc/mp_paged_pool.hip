@@ -101,17 +101,17 @@ __device__ __forceinline__ void map_rows(const PagePool& p, const StepRows& rows
     if (rows.slots) rows.slots[r] = slot;
 }
 
+// Any number of sequences, 1024 after 1024.
 __global__ __launch_bounds__(kThreads) void paged_reserve_kernel(PagePool p, const int32_t* n_new, const int32_t* keep, int32_t* granted, StepRows rows)
 {
     __shared__ Shared sm;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     int32_t* const stack = p.free_pages;
     uint32_t top = (uint32_t)min(max(p.n_free[0], 0), p.n_pages);
-    Sequence seq{};
     // Pages that go back.
     int turn = 0;
     for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
-        seq = sequence_at(p, keep, s0 + tid);
+        const Sequence seq = sequence_at(p, keep, s0 + tid);
         uint32_t all;
         const uint32_t incl = block_scan(sm, 0, (uint32_t)(seq.had - seq.left), &all);
         sm.upto[tid] = incl;
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void paged_reserve_kernel(PagePool p, con
     if (tid == 0) p.q_start[0] = 0;
     for (int s0 = 0; s0 < p.n_seqs; s0 += kThreads) {
         const int b = s0 + tid;
-        if (p.n_seqs > kThreads) seq = sequence_at(p, keep, b);
+        const Sequence seq = sequence_at(p, keep, b);
         const int room = p.table_stride << p.page_shift;
         int come = b < p.n_seqs ? max(n_new[b], 0) : 0;
         if (come > room - seq.stay) come = 0;
