@@ -97,7 +97,7 @@ mp_status cache_ok(const char* who, const mp_paged_kv* c, PagedKv* out)
     return MP_OK;
 }
 
-// `count` of `bytes` each; a null pointer overlaps nothing.
+// `count` of `bytes` each; a null pointer, or none of them, overlaps nothing.
 struct Span {
     const void* p;
     long long count;
@@ -106,7 +106,7 @@ struct Span {
 bool overlap(const Span& a, const Span& b)
 {
     const uintptr_t a0 = (uintptr_t)a.p, a1 = a0 + (uintptr_t)(a.count * a.bytes), b0 = (uintptr_t)b.p, b1 = b0 + (uintptr_t)(b.count * b.bytes);
-    return a.p && b.p && a0 < b1 && b0 < a1;
+    return a.p && b.p && a0 < a1 && b0 < b1 && a0 < b1 && b0 < a1;
 }
 // Whether a result lies on something that is read, or on another result.
 template <int kResults, int kRead>

@@ -81,3 +81,10 @@ def test_arrays_that_meet_do_not_overlap(mp):
     c = _cache(mp)
     for keep in (LEN + 4 * SEQS, START - 4 * SEQS):
         assert mp.lib().mp_paged_tree_keep(C.addressof(c), MASK, WORDS, TOKENS, IN, keep, None) == mp.MP_EHIP
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are no memory: without a GPU the launch itself fails")
+def test_no_rows_overlap_nothing(mp):
+    pool = mp.MpPagePoolArgs(TABLE, LEN, START, K, V, 9, 16, SEQS, COLUMNS)
+    for at in (START + 8, LEN, IN):
+        assert mp.lib().mp_paged_reserve(C.addressof(pool), IN, None, None, at, None, None, 0, None) == mp.MP_EHIP
