@@ -577,7 +577,7 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
  * read), MP_EHIP.
  *
  * mp_paged_tree_attention -- every new token attends the keys of its sequence that are older than the new ones, and the new ones that its mask marks (any, also
- * such as stand behind it; itself only if it is marked).  window: of all these, the last `window` keys (marks, whether or not their pages are
+ * such as stand behind it; itself only if it is marked; none past max_new).  window: of all these, the last `window` keys (marks, whether or not their pages are
  * there, count first).  Other arguments, workspace, results and errors as of mp_paged_attention; probabilities have two parts where max_new * G <= 32, and in large batches with max_new * G > 128 for
  * sequences of up to 16 query rows a KV head.
  *

@@ -5,7 +5,8 @@
 // sequence; the first that finds too few gets no tokens, and neither does any behind it that needs pages.
 //
 // One workgroup, for everything hangs on two running sums over the sequences: bound by its trips to memory one behind the other.  The maps of many tokens are a launch of their own.  64 sequences of up to
-// eight tokens 4.8 us; 512 of which 64 give 4096 pages back and take as many 9.2, and 3.6 for the maps of their 50 thousand rows.
+// eight tokens 4.8 us; 512 that give 3183 pages back, most of them 64 sequences', and take as many 8.9 to 9.2, and 3.5 for the maps of their 50 thousand rows.  A call, with eight tokens each of as many
+// sequences and no maps: 1024 5.7 us; past that, in turns of 1024 without what LDS hands on, 1025 7.4, 2048 8.0, 4096 14.0.
 #include "mp_device.h"
 #include "mp_launch.h"
 #include "mp_paged.h"
@@ -223,7 +224,7 @@ struct SharedOnce {
     uint32_t taken;
     int32_t back[kKept], fresh[kKept];
 };
-// The first of the ascending sums that lies behind x, or the last of 2 half (half: a power of two, or 0).  (For 4096 entries, searches of several at a time, step by step, took LDS longer than they
+// The first of the ascending sums that lies behind x, or the last of 2 half (half: a power of two, or 0).  (For 3183 entries, searches of several at a time, step by step, took LDS longer than they
 // saved in trips to it, 11.9 us for 9.3; marks where sequences begin and a running maximum over them 10.3.)
 __device__ __forceinline__ int first_behind(const uint32_t* sums, int half, uint32_t x)
 {

@@ -5,7 +5,8 @@
 // its own, so nothing is put together in the workgroup.  Bound by memory, or by trips to it and to instructions: a third of the code of mp_paged_token.hip for 64 rows, where each wave has all rows and keys of its own.
 //
 // By this and by what ran before (that one up to 64 rows, mp_paged_chunk.hip), 8 KV heads of four, us: 12 tokens over 4096 keys 16.8 and 22.4, 24 over as many 20 and 23.6; 12 each of 8 sequences of up to 30K 81 and
-// 87 (5.4 TB/s), 24 each 106 and 124, 32 each 91 and 102; 12 each of 32 of up to 2K 38 and 62, 24 each 46.8 and 46.9.  Two groups of rows a wave, for up to 256, took 8 to 10 % longer than chunks.
+// 87 (5.4 TB/s), 24 each 106 and 124, 32 each 91 and 102; 12 each of 32 of up to 2K 38 and 62, 24 each 46.8 and 46.9 (lengths
+// are drawn anew for each number of tokens, so that those of 32 each hold less than those of 24).  Two groups of rows a wave, for up to 256, took 8 to 10 % longer than chunks.
 #include "mp_paged_tile.h"
 
 namespace mp {
@@ -300,6 +301,9 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void paged_tree_rows_kerne
                             for (int e = 0; e < 4; ++e) o[d][e] *= f;
                     }
                     const float shift = m == -INFINITY ? 0.f : m;
+                    // Probabilities are rounded to bf16 once (2^-8, as much as the results are), as of the causal form for more than 32 rows; their sum is that of the unrounded ones.  Error against 64
+                    // bits 0.0021 (0.0016 where they have two parts, up to 32 rows).  Two parts here: 12 tokens over 4096 keys 16.3 -> 16.6 us, 12 each of 8 sequences of up to 30K 87.7 -> 93.8, 24
+                    // each 105 -> 124.
                     bf16x8 p[2];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {

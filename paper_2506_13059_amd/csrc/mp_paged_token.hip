@@ -623,7 +623,10 @@ hipError_t launch(const A& a, float* room, hipStream_t s)
 
 }  // namespace
 
-constexpr int kManyItems = 128;      // sequences times KV heads
+// Sequences times KV heads from which on the merge for few parts runs.  Whole calls by that for many parts and by that for few, us, sequences of up to 2K, 12 and 24 tokens each, 8 KV heads of four: 16
+// items 14.1 and 14.0, 19.2 and 17.9; 64 items 23.4 and 22.2, 32.5 and 29.8; 128 items 32.6 and 30.1, 42.4 and 37.4; 256 items 40.1 and 36.7, 53.1 and 46.6.  The line lies where it is safe rather
+// than where they meet: one sequence over 4096 keys, 8 items, is the case above that loses.
+constexpr int kManyItems = 128;
 
 template <int kGroups>
 static hipError_t merge(const PagedAttention& a, const float* parts, const Cut* cuts, hipStream_t s)
