@@ -466,7 +466,7 @@ typedef struct {
     void* v_pages;               /* likewise                                                          */
     const int32_t* page_table;   /* device int32 [n_seqs, table_stride]                               */
     const int32_t* kv_len;       /* device int32 [n_seqs]: keys of each sequence, the new ones among them */
-    const int32_t* q_start;      /* device int32 [n_seqs + 1]                                         */
+    const int32_t* q_start;      /* device int32 [n_seqs + 1]; n_seqs up to 2^31 - 1025               */
     int32_t n_pages;
     int32_t page_size;           /* a power of two, 1 .. 1024                                         */
     int32_t n_kv_heads;

@@ -21,6 +21,7 @@ constexpr long long kMostRows = 4ll * 0x7fffffff;
 constexpr long long kMostGroups = (1ll << 24) - 1;      // workgroups of 256: a launch counts its lanes in 32 bits
 constexpr long long kMostTokens = 4 * kMostGroups;      // ... where every token has a wave
 constexpr int kMostSequences = (1 << 22) - 1;                // ... of up to 1024 lanes each
+constexpr int kMostTurns = 0x7fffffff - 1024;                // sequences are gone through up to 1024 at a time, in 32 bits
 
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -81,6 +82,7 @@ mp_status cache_ok(const char* who, const mp_paged_kv* c, PagedKv* out)
         return fail(nullptr, MP_EINVAL, "%s: page_size %d is not a power of two up to 1024", who, c->page_size);
     if ((long long)c->table_stride * c->page_size > kMostKeys)
         return fail(nullptr, MP_EINVAL, "%s: a sequence's pages hold more than 2^31 - 1 keys", who);
+    if (c->n_seqs > kMostTurns) return fail(nullptr, MP_EINVAL, "%s: too many sequences", who);
     if (!c->k_pages || !c->v_pages) return fail(nullptr, MP_EINVAL, "%s: null pages", who);
     if (!aligned(c->k_pages) || !aligned(c->v_pages)) return fail(nullptr, MP_EINVAL, "%s: pages do not start on 16 bytes", who);
     if (c->n_seqs > 0 && (!c->page_table || !c->kv_len || !c->q_start)) return fail(nullptr, MP_EINVAL, "%s: null page_table, kv_len or q_start", who);
@@ -386,8 +388,8 @@ mp_status mp_paged_reserve(const mp_page_pool* pool, const int32_t* n_new, const
     if (pool->n_seqs > 0 && (!pool->page_table || !pool->kv_len || !n_new)) return fail(nullptr, MP_EINVAL, "%s: null page_table, kv_len or n_new", who);
     if (n_rows < 0) return fail(nullptr, MP_EINVAL, "%s: n_rows %d < 0", who, n_rows);
     if (!sequence && !positions && !slots) n_rows = 0;
-    // (sequences are gone through 1024 and rows 64 at a time, in 32 bits; a row of 2^31 - 1 would lie before no start)
-    if (n_rows > kMostKeys - 64 || pool->n_seqs > kMostKeys - 1024) return fail(nullptr, MP_EINVAL, "%s: too many rows or sequences", who);
+    // (rows are gone through 64 at a time; one of 2^31 - 1 would lie before no start)
+    if (n_rows > kMostKeys - 64 || pool->n_seqs > kMostTurns) return fail(nullptr, MP_EINVAL, "%s: too many rows or sequences", who);
     const long long n = pool->n_seqs;
     if (overlap({{pool->page_table, n * pool->table_stride, 4}, {pool->kv_len, n, 4}, {pool->q_start, n + 1, 4}, {pool->free_pages, pool->n_pages, 4}, {pool->n_free, 1, 4},
                  {granted, n, 4}, {sequence, n_rows, 4}, {positions, n_rows, 4}, {slots, n_rows, 8}},
